@@ -355,6 +355,122 @@ int llama_stack_train_step(const void* x, const void* const* params, const void*
                            void* dx, float* const* grads, int n_layers, int S, int d_model,
                            int n_heads, int d_ff, int n_hosts, int causal, hipStream_t stream);
 
+/*
+ * A decode step over a paged key/value cache, for a batch of requests of different lengths.
+ *
+ * The cache is n_pages pages of page_size tokens: k_pages, v_pages [n_pages, page_size, Hkv, D].
+ * Request r owns the pages its row of block_table int32 [R, max_pages] lists, in order; its token
+ * at position p lies in slot block_table[r][p / page_size] * page_size + p % page_size.  The new
+ * tokens of a step lie packed in T rows, request after request; cu_rows[r] is the first row of
+ * request r, cu_rows[R] their number; T may be larger, rows from there on are padding.
+ *   paged_plan         pages for the new tokens, cu_rows, slots and positions of the rows
+ *   paged_append       rotary embedding of q and k; k and v into their slots
+ *   paged_attn_decode  attention of the new tokens over each request's pages
+ * kv_type:
+ *   RA_KV_BF16  pages hold bf16; k_scales, v_scales NULL
+ *   RA_KV_E4M3  pages hold 8-bit floats (OCP e4m3) and k_scales, v_scales uint8 [n_pages,
+ *               page_size, Hkv] the exponents of their scales: element times 2^(scale - 127).
+ *               paged_append takes the smallest power of two with which every finite element of
+ *               the token's head is at most 448 in magnitude, 2^-126 at least (1 where all are
+ *               zero), so that what a page stands for is exact in bf16 (above bf16's smallest
+ *               numbers).  e4m3 has no infinity: infinite elements are stored as NaN.  Scales
+ *               are 1 .. 254.
+ * page_size: a power of two, at most 1024; n_pages * page_size < 2^31; R <= 4096; heads <= 1024;
+ * D in {64, 128}.  Device-side integers are not trusted: what lies out of range is left out, as
+ * said at each call, and nothing out of bounds is read or written.
+ */
+typedef enum { RA_KV_BF16 = 0, RA_KV_E4M3 = 1 } ra_kv;
+
+/* Flags that paged_plan leaves in counts[3]. */
+enum {
+  RA_PLAN_PAGES = 1,     /* the free list ran out */
+  RA_PLAN_CAPACITY = 2,  /* a request is longer than max_pages pages */
+  RA_PLAN_ROWS = 4,      /* more new tokens than T rows */
+  RA_PLAN_BAD_INPUT = 8  /* a negative length, number of tokens or free_head (taken as 0) */
+};
+
+/*
+ * Pages, slots and positions of a step's new tokens, on the device (no host synchronisation).
+ *   lens        in  int32 [R]  tokens in the cache;  n_new in int32 [R]  new tokens of this step
+ *   free_pages  in  int32 [n_free]  ids of free pages, taken in order from entry *free_head on
+ *   free_head   in  int32 [1], or NULL for 0; not inside counts
+ *   block_table in/out int32 [R, max_pages]: request r holds ceil(lens[r] / page_size) pages; the
+ *               entries of the pages it needs on top are written, in request order, no others
+ *   cu_rows     out int32 [R + 1]    new_lens out int32 [R] = lens + n_new (not lens itself)
+ *   slots, positions out int32 [T]  of each row; both -1 in padding rows
+ *   counts      out int32 [4]: rows, pages taken, the free_head of the next step, flags
+ * Where the free list runs out, an id in it or an entry held lies outside [0, n_pages) or a
+ * request outgrows max_pages, the entry (if there is one) and the slots of its tokens are -1.
+ * Tokens that T rows do not hold are not taken: cu_rows ends at T, new_lens counts those taken.
+ * Lengths and positions end at 2^31 - 1.
+ * Outputs do not overlap inputs or one another.  Calling again with the same inputs gives the
+ * same outputs.
+ */
+int paged_plan(const int* lens, const int* n_new, const int* free_pages, const int* free_head, int* block_table,
+               int* cu_rows, int* new_lens, int* slots, int* positions, int* counts, int R, int page_size,
+               int max_pages, int n_pages, int n_free, int T, hipStream_t stream);
+
+/*
+ * The new tokens' keys and values into the cache, after the rotary embedding of rope_apply.
+ *   q         in  bf16 [T, Hq, D], k, v in bf16 [T, Hkv, D], rows q_stride, k_stride, v_stride
+ *             elements apart (multiples of 8: they may be parts of one projection's output);
+ *             q and q_out both NULL: keys and values alone
+ *   q_out     out bf16 [T, Hq, D], dense: q rotated (may be q itself where q is dense)
+ *   k_pages, v_pages (and scales) in/out: the slots of the rows are written, nothing else
+ *   slots, positions in int32 [T] (paged_plan).  A row of a negative position is left out; one
+ *             whose slot lies outside the cache has q rotated and nothing stored.  Two rows with
+ *             one slot leave elements of either in it.
+ *   rotate    1: q and k are rotated by their positions (angles formed in double); 0: copied
+ */
+int paged_append(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                 unsigned char* k_scales, unsigned char* v_scales, const int* slots, const int* positions, int T,
+                 int Hq, int Hkv, int D, int q_stride, int k_stride, int v_stride, int n_pages, int page_size,
+                 int kv_type, int rotate, hipStream_t stream);
+
+/*
+ * Attention of the new tokens over their requests' pages: o = softmax(q K^T / sqrt(D)) V, query
+ * head i reading key head i / (Hq / Hkv).
+ *   q          in  bf16 [T, Hq, D];  o out bf16 [T, Hq, D];  lse out f32 [T, Hq]
+ *   lens       in  int32 [R]: tokens in the cache, this step's among them (new_lens of paged_plan)
+ *   cu_rows    in  int32 [R + 1] ascending, or NULL: row r is the one new token of request r
+ *   max_new    the most new tokens of a request, <= 32; later rows of a longer one are not computed
+ *   Row t of the n of request r sits at position lens[r] - n + t and sees keys up to its own.
+ *   Keys past max_pages pages, or in pages outside [0, n_pages), are masked.  A masked key counts
+ *   for nothing, whatever its row holds; a row that sees no key has o = 0, lse = -inf.  Rows of
+ *   no request are left as they are.
+ *   workspace  workspace_bytes of device memory on a 16-byte boundary, or NULL: allocated by the
+ *              library like every other call's.  With a workspace of its own a call allocates
+ *              nothing and can be captured into a HIP graph; calls that may overlap, and graphs
+ *              that may run at once, need one each.  Its contents before the call do not matter.
+ * paged_attn_workspace gives the bytes that calls of this shape (and any lengths) need.
+ */
+int paged_attn_workspace(int R, int Hq, int Hkv, int D, int max_new, size_t* bytes);
+int paged_attn_decode(const void* q, const void* k_pages, const void* v_pages, const unsigned char* k_scales,
+                      const unsigned char* v_scales, const int* block_table, const int* lens, const int* cu_rows,
+                      void* o, float* lse, void* workspace, size_t workspace_bytes, int T, int R, int Hq, int Hkv,
+                      int D, int n_pages, int page_size, int max_pages, int max_new, int kv_type,
+                      hipStream_t stream);
+
+/*
+ * Products of a few rows with weights in 4 bits (blockwise_linear's product, for decode steps):
+ *   y = x W (+ residual);  x in bf16 [T, d_in], residual in bf16 [T, d_out] or NULL, y out bf16
+ * W in the MX format: elements e2m1 (sign bit, then 0, 0.5, 1, 1.5, 2, 3, 4, 6), one scale
+ * 2^(byte - 127) for 32 inputs of an output (byte 1 .. 254; 255 makes the group NaN).  Products
+ * are exact in bf16 operands and summed in float32.  With nb = ceil(d_out / 16), kb =
+ * ceil(d_in / 128):
+ *   w4      uint8 [nb, kb, 64, 16]: byte j of entry l of block (i, b) holds output 16 i + l % 16,
+ *           inputs 128 b + 32 (j / 4) + 8 (l / 16) + 2 (j % 4) (low four bits) and the next (high)
+ *   scales  uint8 [nb, kb, 16, 4]: output 16 i + r, inputs 128 b + 32 g ... + 31
+ * Places past d_out and d_in hold zero codes.  mx4_pack fills both from w bf16 [d_in, d_out]: the
+ * scale is the smallest power of two (2^-126 at least) with which the group is at most 6 in
+ * magnitude, codes are rounded to nearest, ties to the even code; a group with an infinity or NaN
+ * has scale 255.
+ * d_in % 32 == 0, d_in * d_out < 2^31, T <= 512.
+ */
+int mx4_pack(const void* w, void* w4, unsigned char* scales, int d_in, int d_out, hipStream_t stream);
+int mx4_linear(const void* x, const void* w4, const unsigned char* scales, const void* residual, void* y, int T,
+               int d_in, int d_out, hipStream_t stream);
+
 /* Description of the last error returned on the calling thread ("" if none).  Valid
  * until the next library call on that thread. */
 const char* ring_attn_last_error(void);

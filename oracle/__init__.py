@@ -31,6 +31,9 @@ Modules
   layer      -- one transformer layer as Algorithm 1 composes it: projections,
                 ring attention, output projection with residual, blockwise FFN with
                 residual; forward and backward.
+  serving    -- a decode step over a paged key/value cache (page plan, append with rotary
+                embedding and 8-bit rows, attention of requests of different lengths)
+                and 4-bit weights: from the definitions in include/ringattn.h.
   overlap    -- Section 3's arithmetic intensity between hosts: the block size at which
                 a ring step's attention work hides the key/value transfer (c >= F/B) and
                 the minimal sequence per host (6c).

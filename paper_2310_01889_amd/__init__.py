@@ -24,11 +24,14 @@ __all__ = [
     "blockwise_linear", "blockwise_linear_bwd", "ring_layer_fwd", "ring_layer_bwd",
     "rms_norm_fwd", "rms_norm_bwd", "rope_apply", "swiglu_ffn", "swiglu_ffn_bwd",
     "llama_layer_fwd", "llama_layer_bwd", "llama_stack_train_step",
-    "attention_fwd", "attention_bwd", "attention_decode",
+    "paged_plan", "paged_append", "paged_attn_workspace", "paged_attn_decode", "mx4_pack", "mx4_linear",
+    "attention_fwd", "attention_bwd", "attention_decode", "paged_attention", "mx4_weights",
+    "PLAN_PAGES", "PLAN_CAPACITY", "PLAN_ROWS", "PLAN_BAD_INPUT",
     "ACT_GELU_ERF", "ACT_RELU", "ACT_GELU_TANH",
 ]
 
 ACT_GELU_ERF, ACT_RELU, ACT_GELU_TANH = 0, 1, 2
+PLAN_PAGES, PLAN_CAPACITY, PLAN_ROWS, PLAN_BAD_INPUT = 1, 2, 4, 8  # flags in counts[3] of paged_plan
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
@@ -62,6 +65,12 @@ _SIGS = {
     "llama_layer_fwd": [_P] * 3 + [_I] * 6 + [_P],
     "llama_layer_bwd": [_P] * 5 + [_I] * 6 + [_P],
     "llama_stack_train_step": [_P] * 6 + [_I] * 7 + [_P],
+    "paged_plan": [_P] * 10 + [_I] * 6 + [_P],
+    "paged_append": [_P] * 10 + [_I] * 11 + [_P],
+    "paged_attn_workspace": [_I] * 5 + [_P],
+    "paged_attn_decode": [_P] * 11 + [ctypes.c_size_t] + [_I] * 10 + [_P],
+    "mx4_pack": [_P] * 3 + [_I] * 2 + [_P],
+    "mx4_linear": [_P] * 5 + [_I] * 3 + [_P],
 }
 
 
@@ -397,6 +406,144 @@ def llama_stack_train_step(x, layer_params, dz, z, dx, layer_grads, n_heads, n_h
           garr, len(layer_params), S, dm, int(n_heads), dff, int(n_hosts), int(causal), _stream(stream))
 
 
+def _here(*ts):
+    """The tensors must live on the current GPU: its stream runs the call."""
+    d = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.get_device() != d:
+            raise ValueError("tensors must be on the current GPU (cuda:%d), got %s" % (d, t.device))
+
+
+def _sized(t, name, *shape):
+    if tuple(t.shape) != shape:
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def paged_plan(lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts, page_size,
+               n_pages, stream=None):
+    """int32 tensors: lens, n_new, new_lens [R], free_pages [n_free], free_head [1] or None,
+    block_table [R, max_pages], cu_rows [R + 1], slots, positions [T], counts [4]."""
+    R, max_pages = (int(x) for x in block_table.shape)
+    T, i32 = int(slots.shape[0]), torch.int32
+    _here(lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts)
+    for t, name, n in ((lens, "lens", R), (n_new, "n_new", R), (cu_rows, "cu_rows", R + 1), (new_lens, "new_lens", R),
+                       (slots, "slots", T), (positions, "positions", T), (counts, "counts", 4)):
+        _sized(t, name, n)
+    _call("paged_plan", _ptr(lens, i32, "lens"), _ptr(n_new, i32, "n_new"), _ptr(free_pages, i32, "free_pages"),
+          _ptr(free_head, i32, "free_head"), _ptr(block_table, i32, "block_table"), _ptr(cu_rows, i32, "cu_rows"),
+          _ptr(new_lens, i32, "new_lens"), _ptr(slots, i32, "slots"), _ptr(positions, i32, "positions"),
+          _ptr(counts, i32, "counts"), R, int(page_size), max_pages, int(n_pages), int(free_pages.numel()), T,
+          _stream(stream))
+
+
+KV_BF16, KV_E4M3 = 0, 1
+
+
+def _cache(k_pages, v_pages, k_scales, v_scales):
+    """Pointers of a cache's tensors, its kv_type and its shape."""
+    if k_pages.dim() != 4:
+        raise ValueError("expected a [n_pages, page_size, Hkv, D] cache")
+    shape = tuple(int(x) for x in k_pages.shape)
+    _sized(v_pages, "v_pages", *shape)
+    dt = k_pages.dtype
+    if dt not in (torch.bfloat16, torch.float8_e4m3fn):
+        raise TypeError("k_pages must be torch.bfloat16 or torch.float8_e4m3fn, got %s" % dt)
+    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+        if t is not None:
+            _sized(t, name, *shape[:3])
+    u8 = torch.uint8
+    return ((_ptr(k_pages, dt, "k_pages"), _ptr(v_pages, dt, "v_pages"), _ptr(k_scales, u8, "k_scales"),
+             _ptr(v_scales, u8, "v_scales")), KV_BF16 if dt == torch.bfloat16 else KV_E4M3, shape)
+
+
+def _rows(t, name, T, H, D):
+    """Pointer and row stride of a bf16 [T, H, D] tensor whose rows are dense."""
+    _sized(t, name, T, H, D)
+    if t.dtype != torch.bfloat16:
+        raise TypeError("%s must be torch.bfloat16, got %s" % (name, t.dtype))
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor" % name)
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError("the heads of a row of %s must be contiguous" % name)
+    return ctypes.c_void_p(t.data_ptr()), int(t.stride(0)) if T > 1 else H * D
+
+
+def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=None, v_scales=None, rotate=True,
+                 stream=None):
+    """q [T, Hq, D] (or None, with q_out), k, v [T, Hkv, D]: rows may be strided."""
+    T = int(slots.shape[0])
+    ptrs, kind, (n_pages, page_size, Hkv, D) = _cache(k_pages, v_pages, k_scales, v_scales)
+    _here(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales, v_scales)
+    Hq = 0 if q is None else int(q.shape[1])
+    qp, qs = (None, 0) if q is None else _rows(q, "q", T, Hq, D)
+    kp, ks = _rows(k, "k", T, Hkv, D)
+    vp, vs = _rows(v, "v", T, Hkv, D)
+    if q_out is not None:
+        _sized(q_out, "q_out", T, Hq, D)
+    _sized(positions, "positions", T)
+    _call("paged_append", qp, kp, vp, _ptr(q_out, torch.bfloat16, "q_out"), *ptrs, _ptr(slots, torch.int32, "slots"),
+          _ptr(positions, torch.int32, "positions"), T, Hq, Hkv, D, qs, ks, vs, n_pages, page_size, kind,
+          int(bool(rotate)), _stream(stream))
+
+
+def paged_attn_workspace(R, Hq, Hkv, D, max_new):
+    """Bytes of workspace a paged_attn_decode of this shape needs."""
+    n = ctypes.c_size_t(0)
+    _call("paged_attn_workspace", int(R), int(Hq), int(Hkv), int(D), int(max_new), ctypes.byref(n))
+    return n.value
+
+
+def paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, max_new, k_scales=None, v_scales=None,
+                      workspace=None, stream=None):
+    """q, o [T, Hq, D], lse [T, Hq]; cu_rows None: row r is the one new token of request r.
+    workspace: a contiguous GPU tensor of paged_attn_workspace bytes, or None."""
+    if q.dim() != 3:
+        raise ValueError("expected a [T, Hq, D] tensor")
+    T, Hq, D = (int(x) for x in q.shape)
+    ptrs, kind, (n_pages, page_size, Hkv, Dc) = _cache(k_pages, v_pages, k_scales, v_scales)
+    if Dc != D:
+        raise ValueError("head dim %d of q, %d of the cache" % (D, Dc))
+    R, max_pages = (int(x) for x in block_table.shape)
+    _here(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, k_scales, v_scales, workspace)
+    _sized(o, "o", T, Hq, D)
+    _sized(lse, "lse", T, Hq)
+    _sized(lens, "lens", R)
+    if cu_rows is not None:
+        _sized(cu_rows, "cu_rows", R + 1)
+    i32, bf = torch.int32, torch.bfloat16
+    _call("paged_attn_decode", _ptr(q, bf, "q"), *ptrs, _ptr(block_table, i32, "block_table"), _ptr(lens, i32, "lens"),
+          _ptr(cu_rows, i32, "cu_rows"), _ptr(o, bf, "o"), _ptr(lse, torch.float32, "lse"),
+          _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+          T, R, Hq, Hkv, D, n_pages, page_size, max_pages, int(max_new), kind, _stream(stream))
+
+
+def mx4_pack(w, w4, scales, stream=None):
+    K, N = (int(s) for s in w.shape)
+    _here(w, w4, scales)
+    _mx_sized(w4, scales, K, N)
+    _call("mx4_pack", _ptr(w, torch.bfloat16, "w"), _ptr(w4, torch.uint8, "w4"), _ptr(scales, torch.uint8, "scales"),
+          K, N, _stream(stream))
+
+
+def _mx_sized(w4, scales, K, N):
+    nb, kb = -(-N // 16), -(-K // 128)
+    _sized(w4, "w4", nb, kb, 64, 16)
+    _sized(scales, "scales", nb, kb, 16, 4)
+
+
+def mx4_linear(x, w4, scales, residual, y, stream=None):
+    T, K = (int(s) for s in x.shape)
+    N = int(y.shape[1])
+    _here(x, w4, scales, residual, y)
+    _mx_sized(w4, scales, K, N)
+    _sized(y, "y", T, N)
+    if residual is not None:
+        _sized(residual, "residual", T, N)
+    bf, u8 = torch.bfloat16, torch.uint8
+    _call("mx4_linear", _ptr(x, bf, "x"), _ptr(w4, u8, "w4"), _ptr(scales, u8, "scales"),
+          _ptr(residual, bf, "residual"), _ptr(y, bf, "y"), T, K, N, _stream(stream))
+
+
 # ----------------------------------------------------------------------------------
 # Allocating wrappers
 # ----------------------------------------------------------------------------------
@@ -437,3 +584,21 @@ def attention_decode(q, k_cache, v_cache, n_hosts, causal=True):
     lse = torch.empty((B, H, Tq), dtype=torch.float32, device=q.device)
     ring_attn_decode(q, k_cache, v_cache, o, lse, n_hosts, causal)
     return o, lse
+
+
+def paged_attention(q, k_pages, v_pages, block_table, lens, cu_rows=None, max_new=1, k_scales=None, v_scales=None):
+    """Returns (o [T, Hq, D] bf16, lse [T, Hq] f32) of paged_attn_decode, zeros in padding rows."""
+    o = torch.zeros_like(q)
+    lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+    paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, max_new, k_scales, v_scales)
+    return o, lse
+
+
+def mx4_weights(w):
+    """Returns (w4, scales) of mx4_pack for a bf16 [d_in, d_out] weight."""
+    K, N = (int(s) for s in w.shape)
+    nb, kb = -(-N // 16), -(-K // 128)
+    w4 = torch.empty((nb, kb, 64, 16), dtype=torch.uint8, device=w.device)
+    scales = torch.empty((nb, kb, 16, 4), dtype=torch.uint8, device=w.device)
+    mx4_pack(w, w4, scales)
+    return w4, scales

@@ -1,0 +1,367 @@
+// A decode step over a paged key/value cache: the plan (pages, slots and positions of the new
+// tokens), and the append that rotates q and k and writes keys and values into their pages.
+//
+// The cache is n_pages pages of page_size tokens; request r owns the pages its row of
+// block_table lists, in order, so its token at position p lies in slot
+//   block_table[r][p / page_size] * page_size + p % page_size.
+// The attention over these pages is in paged_attn.hip.
+#include <math.h>
+
+#include "ra_common.h"
+#include "ra_paged.h"
+#include "ra_runtime.h"
+#include "ringattn.h"
+
+namespace ra {
+namespace {
+
+// ---- plan ----------------------------------------------------------------------------------
+constexpr int kPlanMaxR = kMaxRequests;  // their two prefix sums stay in LDS
+constexpr int kPlanThreads = 256;
+constexpr int kPlanRows = 4;     // rows a thread
+
+struct PlanArgs {
+  const int *lens, *n_new, *free_pages, *free_head;
+  int *table, *cu, *new_lens, *slots, *positions, *counts;
+  int R, page_shift, max_pages, n_pages, n_free, T;
+};
+
+// Exclusive prefix sum over the workgroup's threads; *total is the sum of all.
+__device__ __forceinline__ long long block_scan(long long v, long long* total, long long* s_wave) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const long long y = __shfl_up(x, off);
+    if (lane >= off) x += y;
+  }
+  __syncthreads();  // an earlier scan's sums have been read
+  if (lane == 63) s_wave[wave] = x;
+  __syncthreads();
+  long long before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) before += s_wave[w];
+    all += s_wave[w];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// Every workgroup forms the prefix sums of all requests' rows and pages (R is small and the
+// lengths stay in L2), then fills its share of the rows and of the requests' table entries: one
+// launch, no order between workgroups.  A new page's id is free_pages[head + its number in
+// request order], so nothing here depends on what another workgroup writes.
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PlanArgs a) {
+  __shared__ int s_cu[kPlanMaxR + 1];    // first row of each request
+  __shared__ int s_page[kPlanMaxR + 1];  // number of its first new page (at most n_free)
+  __shared__ long long s_wave[kPlanThreads / 64];
+  const int tid = threadIdx.x;
+  const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
+  const int r0 = min(a.R, tid * per), r1 = min(a.R, r0 + per);
+  const int P = 1 << a.page_shift;
+  const long long cap = (long long)a.max_pages << a.page_shift;
+  int flags = 0;
+  const int head_in = a.free_head ? *a.free_head : 0;
+  if (head_in < 0) flags |= RA_PLAN_BAD_INPUT;
+  const int head = min(max(head_in, 0), a.n_free);
+
+  // rows: a request takes no more of them than T holds
+  long long sum = 0, all_rows, total;
+  for (int r = r0; r < r1; ++r) {
+    const int n = a.n_new[r];
+    if (n < 0) flags |= RA_PLAN_BAD_INPUT;
+    sum += max(n, 0);
+  }
+  long long at = block_scan(sum, &all_rows, s_wave);
+  for (int r = r0; r < r1; ++r) {
+    s_cu[r] = (int)min(at, (long long)a.T);
+    at += max(a.n_new[r], 0);
+  }
+  if (tid == 0) s_cu[a.R] = (int)min(all_rows, (long long)a.T);
+  if (all_rows > a.T) flags |= RA_PLAN_ROWS;
+  __syncthreads();
+
+  auto held = [&](long long tokens) { return (int)((min(tokens, cap) + P - 1) >> a.page_shift); };
+  sum = 0;
+  for (int r = r0; r < r1; ++r) {
+    const int len = a.lens[r];
+    if (len < 0) flags |= RA_PLAN_BAD_INPUT;
+    const long long before = max(len, 0), after = before + s_cu[r + 1] - s_cu[r];
+    if (after > cap) flags |= RA_PLAN_CAPACITY;
+    sum += held(after) - held(before);
+  }
+  at = block_scan(sum, &total, s_wave);
+  for (int r = r0; r < r1; ++r) {
+    s_page[r] = (int)min(at, (long long)a.n_free);
+    const long long before = max(a.lens[r], 0), after = before + s_cu[r + 1] - s_cu[r];
+    at += held(after) - held(before);
+  }
+  const long long left = a.n_free - head;
+  if (total > left) flags |= RA_PLAN_PAGES;
+  __syncthreads();
+
+  auto fresh_page = [&](int r, int nth) {  // id of the nth new page of request r, or -1
+    const long long i = (long long)head + s_page[r] + nth;
+    const int id = i < a.n_free ? a.free_pages[i] : -1;
+    return id >= 0 && id < a.n_pages ? id : -1;
+  };
+
+  // table entries, offsets and lengths of this workgroup's requests
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const long long before = max(a.lens[r], 0), after = before + s_cu[r + 1] - s_cu[r];
+    const int h0 = held(before), h1 = held(after);
+    for (int j = h0 + tid; j < h1; j += kPlanThreads) a.table[(long long)r * a.max_pages + j] = fresh_page(r, j - h0);
+    if (tid == 0) {
+      a.cu[r] = s_cu[r];
+      a.new_lens[r] = (int)min(after, 0x7fffffffll);
+    }
+  }
+
+  // slots and positions of its rows
+  const int rows = s_cu[a.R];
+  const long long i0 = ((long long)blockIdx.x * kPlanThreads + tid) * kPlanRows;
+  if (i0 < a.T) {
+    int lo = 0, hi = a.R - 1;  // the last request that starts at or before row i0
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_cu[mid] <= i0) lo = mid; else hi = mid - 1;
+    }
+    int r = lo;
+    for (int e = 0; e < kPlanRows; ++e) {
+      const int i = (int)i0 + e;
+      if (i >= a.T) break;
+      int slot = -1, pos = -1;
+      if (i < rows) {
+        while (s_cu[r + 1] <= i) ++r;
+        const long long before = max(a.lens[r], 0), p = before + i - s_cu[r];
+        pos = (int)min(p, 0x7fffffffll);
+        if (p < cap) {
+          const int j = (int)(p >> a.page_shift), h0 = held(before);
+          const int id = j < h0 ? a.table[(long long)r * a.max_pages + j] : fresh_page(r, j - h0);
+          if (id >= 0 && id < a.n_pages) slot = (id << a.page_shift) + (int)(p & (P - 1));
+        }
+      }
+      a.slots[i] = slot;
+      a.positions[i] = pos;
+    }
+  }
+
+  if (blockIdx.x == 0) {
+    __shared__ int s_flags[kPlanThreads / 64];
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) flags |= __shfl_xor(flags, off);
+    if ((tid & 63) == 0) s_flags[tid >> 6] = flags;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < kPlanThreads / 64; ++w) flags |= s_flags[w];
+      const int took = (int)min(total, left);
+      a.cu[a.R] = rows;
+      a.counts[0] = rows;
+      a.counts[1] = took;
+      a.counts[2] = head + took;
+      a.counts[3] = flags;
+    }
+  }
+}
+
+// ---- append --------------------------------------------------------------------------------
+constexpr double kRopeBase = 10000.0;
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+
+struct RopeFreq {
+  double turns[64];  // base^(-2i/D) / (2 pi), i < D/2: turns a position
+};
+
+struct AppendArgs {
+  const bf16 *q, *k, *v;
+  bf16* q_out;
+  void *k_pages, *v_pages;
+  uint8_t *k_scales, *v_scales;
+  const int *slots, *positions;
+  int T, Hq, Hkv, q_stride, k_stride, v_stride, rotate;
+  long long n_slots;
+};
+
+// A workgroup takes TB tokens: the cosines and sines of their positions go to LDS first, then 8
+// elements a thread of every head.  Angles: the turns position * freq in double, the whole turns
+// dropped, then sine and cosine of the rest in float32 (positions reach 10^6 radians and more).
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, const RopeFreq f, int TB) {
+  constexpr int CPR = D / 8;  // threads a head
+  extern __shared__ float s_rope[];  // [TB][D/2][2]: cos, sin
+  const int t0 = blockIdx.x * TB, nt = min(TB, a.T - t0);
+  if (a.rotate)
+    for (int i = threadIdx.x; i < nt * (D / 2); i += 256) {
+      const double turns = (double)a.positions[t0 + i / (D / 2)] * f.turns[i % (D / 2)];
+      const float part = (float)(turns - rint(turns));
+      float sn, cs;
+      sincospif(2.f * part, &sn, &cs);
+      s_rope[2 * i] = cs;
+      s_rope[2 * i + 1] = sn;
+    }
+  __syncthreads();
+  const int heads = a.Hq + 2 * a.Hkv;
+  const int items = nt * heads * CPR;
+  // whole waves run the loop, so that the lanes of a head reduce together
+  for (int base = 0; base < items; base += 256) {
+    const int it = base + threadIdx.x;
+    const bool on = it < items;
+    const int ch = it % CPR, hh = on ? it / CPR % heads : 0, tl = on ? it / (CPR * heads) : 0, t = t0 + tl;
+    const int pos = a.positions[t], slot = a.slots[t];
+    const bool is_q = hh < a.Hq, is_k = !is_q && hh < a.Hq + a.Hkv;
+    const int h = is_q ? hh : is_k ? hh - a.Hq : hh - a.Hq - a.Hkv;
+    const bool live = on && pos >= 0 && (is_q ? a.q != nullptr : slot >= 0 && slot < a.n_slots);
+    float x[8];
+    if (live) {
+      const bf16* src = is_q ? a.q + (long long)t * a.q_stride
+                             : is_k ? a.k + (long long)t * a.k_stride : a.v + (long long)t * a.v_stride;
+      const bf16x8 in = *(const bf16x8*)(src + h * D + ch * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)in[e];
+      if (a.rotate && (is_q || is_k)) {
+        const float* cs = s_rope + tl * D + ch * 8;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x0 = x[2 * e], x1 = x[2 * e + 1], c = cs[2 * e], s = cs[2 * e + 1];
+          x[2 * e] = x0 * c - x1 * s;
+          x[2 * e + 1] = x0 * s + x1 * c;
+        }
+      }
+    }
+    const long long row = (long long)slot * a.Hkv + h;
+    if (E4M3 && !is_q) {
+      // scale: the smallest power of two that brings every finite element to at most 448
+      float top = 0.f;
+      if (live) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float m = fabsf(x[e]);
+          if (m < INFINITY) top = fmaxf(top, m);
+        }
+      }
+      uint32_t mag = __float_as_uint(top);
+#pragma unroll
+      for (int off = CPR / 2; off >= 1; off >>= 1) mag = max(mag, (uint32_t)__shfl_xor((int)mag, off));
+      if (live) {
+        // 448 = 1.75 * 2^8: the exponent less 8, one more where the mantissa is past 1.75
+        int e2 = (int)(mag >> 23) - 127 - 8 + ((mag & 0x7fffffu) > 0x600000u);
+        e2 = mag == 0 ? 0 : max(e2, -126);
+        const float inv = ldexpf(1.f, -e2);
+        uint32_t w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          int p = 0;
+          p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j] * inv, x[4 * j + 1] * inv, p, false);
+          p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2] * inv, x[4 * j + 3] * inv, p, true);
+          w[j] = (uint32_t)p;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)  // e4m3 has no infinity: NaN
+            if (!(fabsf(x[4 * j + e]) < INFINITY)) w[j] |= 0x7fu << (8 * e);
+        }
+        uint8_t* out = (uint8_t*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
+        *(u32x2*)out = u32x2{w[0], w[1]};
+        if (ch == 0) (is_k ? a.k_scales : a.v_scales)[row] = (uint8_t)(e2 + 127);
+      }
+    } else if (live) {
+      bf16* out = is_q ? a.q_out + ((long long)t * a.Hq + h) * D + ch * 8
+                       : (bf16*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
+      *(u32x4*)out = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                           pack_bf16x2(x[6], x[7])};
+    }
+  }
+}
+
+const RopeFreq& rope_freq(int D) {
+  struct Tables {
+    RopeFreq f[2];
+    Tables() {
+      for (int d = 0; d < 2; ++d)
+        for (int i = 0; i < 64; ++i) f[d].turns[i] = pow(kRopeBase, -2.0 * i / (64 << d)) / kTwoPi;
+    }
+  };
+  static const Tables t;
+  return t.f[D == 128];
+}
+
+}  // namespace
+
+int check_pages(int page_size, int n_pages, int Hkv, int D) {
+  if (page_size <= 0 || n_pages <= 0 || Hkv <= 0 || D <= 0)
+    return set_err(RA_EINVAL, "sizes must be positive (page_size=%d n_pages=%d Hkv=%d D=%d)", page_size, n_pages, Hkv,
+                   D);
+  if (page_size > kMaxPage || (page_size & (page_size - 1)))
+    return set_err(RA_EUNSUPPORTED, "page_size=%d must be a power of two of at most %d", page_size, kMaxPage);
+  if ((long long)n_pages * page_size >= (1ll << 31))
+    return set_err(RA_EUNSUPPORTED, "n_pages*page_size = %lld slots exceeds 2^31-1", (long long)n_pages * page_size);
+  return RA_OK;
+}
+
+int check_kv(int kv_type, const void* k_scales, const void* v_scales) {
+  if (kv_type != RA_KV_BF16 && kv_type != RA_KV_E4M3)
+    return set_err(RA_EINVAL, "kv_type=%d must be RA_KV_BF16 or RA_KV_E4M3", kv_type);
+  if (kv_type == RA_KV_E4M3 && (!k_scales || !v_scales)) return set_err(RA_EINVAL, "an e4m3 cache needs scales");
+  if (kv_type == RA_KV_BF16 && (k_scales || v_scales)) return set_err(RA_EINVAL, "a bf16 cache has no scales");
+  return RA_OK;
+}
+
+}  // namespace ra
+
+using namespace ra;
+
+extern "C" int paged_plan(const int* lens, const int* n_new, const int* free_pages, const int* free_head,
+                          int* block_table, int* cu_rows, int* new_lens, int* slots, int* positions, int* counts, int R,
+                          int page_size, int max_pages, int n_pages, int n_free, int T, hipStream_t stream) {
+  g_err.clear();
+  if (!lens || !n_new || !free_pages || !block_table || !cu_rows || !new_lens || !slots || !positions || !counts)
+    return set_err(RA_EINVAL, "null pointer argument");
+  if (int e = check_aligned({}, {lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions,
+                                 counts}))
+    return e;
+  if (lens == new_lens || n_new == new_lens) return set_err(RA_EINVAL, "new_lens must not be lens or n_new");
+  if (free_head && free_head >= counts && free_head < counts + 4)
+    return set_err(RA_EINVAL, "free_head must not lie in counts");
+  if (R <= 0 || max_pages <= 0 || n_free <= 0 || T <= 0)
+    return set_err(RA_EINVAL, "sizes must be positive (R=%d max_pages=%d n_free=%d T=%d)", R, max_pages, n_free, T);
+  if (int e = check_pages(page_size, n_pages, 1, 1)) return e;
+  if (R > kPlanMaxR) return set_err(RA_EUNSUPPORTED, "R=%d exceeds %d requests", R, kPlanMaxR);
+  PlanArgs a{lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts, R, 0,
+             max_pages, n_pages, n_free, T};
+  while ((1 << a.page_shift) < page_size) ++a.page_shift;
+  const int per = kPlanThreads * kPlanRows;
+  const unsigned grid = (unsigned)(((long long)T + per - 1) / per);
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(grid), dim3(kPlanThreads), 0, stream, a);
+  RA_HIP(hipGetLastError());
+  return RA_OK;
+}
+
+extern "C" int paged_append(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
+                            unsigned char* k_scales, unsigned char* v_scales, const int* slots, const int* positions,
+                            int T, int Hq, int Hkv, int D, int q_stride, int k_stride, int v_stride, int n_pages,
+                            int page_size, int kv_type, int rotate, hipStream_t stream) {
+  g_err.clear();
+  if (!k || !v || !k_pages || !v_pages || !slots || !positions) return set_err(RA_EINVAL, "null pointer argument");
+  if (!q != !q_out) return set_err(RA_EINVAL, "q and q_out are given together or not at all");
+  if (int e = check_aligned({q, k, v, q_out, k_pages, v_pages}, {slots, positions})) return e;
+  if (int e = check_kv(kv_type, k_scales, v_scales)) return e;
+  if (rotate != 0 && rotate != 1) return set_err(RA_EINVAL, "rotate must be 0 or 1 (got %d)", rotate);
+  if (T <= 0 || Hq < 0 || (q && Hq == 0)) return set_err(RA_EINVAL, "sizes must be positive (T=%d Hq=%d)", T, Hq);
+  if (int e = check_pages(page_size, n_pages, Hkv, D)) return e;
+  if (D != 64 && D != 128) return set_err(RA_EUNSUPPORTED, "head dim D=%d not supported (64 or 128)", D);
+  if (!q) Hq = 0;
+  if (Hq > kMaxHeads || Hkv > kMaxHeads)
+    return set_err(RA_EUNSUPPORTED, "Hq=%d, Hkv=%d: at most %d heads", Hq, Hkv, kMaxHeads);
+  if ((q && (q_stride < Hq * D || q_stride % 8)) || k_stride < Hkv * D || k_stride % 8 || v_stride < Hkv * D ||
+      v_stride % 8)
+    return set_err(RA_EINVAL, "row strides %d, %d, %d must hold the heads and be multiples of 8", q_stride, k_stride,
+                   v_stride);
+  if (q == q_out && q && q_stride != Hq * D) return set_err(RA_EINVAL, "q_out is dense: it can be q only where q is");
+  AppendArgs a{(const bf16*)q, (const bf16*)k, (const bf16*)v, (bf16*)q_out, k_pages, v_pages, k_scales, v_scales,
+               slots, positions, T, Hq, Hkv, q_stride, k_stride, v_stride, rotate, (long long)n_pages * page_size};
+  const int TB = 1;
+  auto* kern = D == 128 ? (kv_type == RA_KV_E4M3 ? paged_append_kernel<128, true> : paged_append_kernel<128, false>)
+                        : (kv_type == RA_KV_E4M3 ? paged_append_kernel<64, true> : paged_append_kernel<64, false>);
+  hipLaunchKernelGGL(kern, dim3((T + TB - 1) / TB), dim3(256), TB * D * 4, stream, a, rope_freq(D), TB);
+  RA_HIP(hipGetLastError());
+  return RA_OK;
+}

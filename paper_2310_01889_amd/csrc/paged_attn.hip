@@ -1,10 +1,23 @@
-// Attention of the newest tokens of many requests over a paged key/value cache.
+// Attention of the newest tokens of many requests over a paged key/value cache, for gfx950.
 //
 // o = softmax(q K^T / sqrt(D)) V over the keys of each request, read page by page through its
 // row of the block table; the new tokens are the last of the cache and see keys up to their own.
+// A step reads every key and value once, 2 D bytes a key and head each (D and a scale in 8 bits):
+// it is bound by HBM bandwidth, as long as the reads are spread evenly over the chip.
+//
+// Work is counted in units: one tile of KT keys of one key head of one request, for up to 32
+// query slots (slot n = new token n / G, query head n % G of the G that share the key head;
+// requests of more slots take several rounds over their keys).  The units of all requests stand
+// in one row, request by request, head by head, and kWorkers waves take equal shares of it, so
+// the lengths of a batch do not matter for the balance.  The lengths are on the device: each
+// wave finds its share from their prefix sums itself.  A wave whose share holds a whole (request,
+// head) writes its result; the others leave partial softmax states that a second launch joins.
 #include <math.h>
 
+#include <algorithm>
+
 #include "ra_common.h"
+#include "ra_dma.h"
 #include "ra_paged.h"
 #include "ra_runtime.h"
 #include "ringattn.h"
@@ -12,94 +25,496 @@
 namespace ra {
 namespace {
 
-constexpr int kMaxNew = 32;  // new tokens a request
+constexpr int kMaxNew = 32;      // new tokens a request
+constexpr int kSlots = 32;       // query slots a wave
+constexpr int kWorkers = 1024;   // waves: one a SIMD
+constexpr int kMinShare = 1;     // units a wave takes at least
+constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
+
+// What the second launch joins: the parts of a group of units (request, key head, round) that
+// several waves share, written by the first of them.  parts = 0: nothing to join.
+struct Split {
+  int row0;   // first q row of the request
+  int h;      // key head
+  int slot0;  // first query slot (of the request's n * G)
+  int slots;  // query slots
+  int first;  // index of the first wave's part; those of the waves after it follow, 2 apart
+  int parts;
+};
 
 struct PagedArgs {
   const bf16* q;  // [T, Hq, D]
   const void *k, *v;
   const uint8_t *ks, *vs;
   const int *table, *lens, *cu;
-  bf16* o;     // [T, Hq, D]
-  float* lse;  // [T, Hq]
+  bf16* o;          // [T, Hq, D]
+  float* lse;       // [T, Hq]
+  float* part_acc;  // [waves][2][M][D] unnormalised outputs: of a wave's first group, of its last
+  float* part_ml;   // [waves][2][M][2] maxima (log2 units) and denominators
+  Split* split;     // one a group where the groups are fewer than the waves, else one a wave
   int T, R, Hq, Hkv, n_pages, page_shift, max_pages, max_new;
+  int M;            // query slots of a group at most
+  int rounds;       // rounds of slots of a request at most
+  int by_group;     // entries of split: 1 a group, 0 a wave
   float scale;
 };
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+// The requests' shape as every wave reads it, whatever the arrays hold.
+struct Request {
+  int row0, n, keys, first;  // first q row, new tokens, keys to read, position of the first new token
+};
+// (The arrays are constant while the kernel runs: scalar loads where r is uniform.)
+typedef __attribute__((address_space(4))) const int const_int;
+__device__ __forceinline__ Request request(const PagedArgs& a, int r) {
+  Request q;
+  int row1 = r + 1;
+  q.row0 = r;
+  if (a.cu) {
+    q.row0 = min(max(((const_int*)a.cu)[r], 0), a.T);
+    row1 = min(max(((const_int*)a.cu)[r + 1], q.row0), a.T);
+  }
+  const int len = max(((const_int*)a.lens)[r], 0), rows = row1 - q.row0;
+  q.n = min(rows, a.max_new);
+  q.first = len - rows;
+  q.keys = (int)min((long long)len, (long long)a.max_pages << a.page_shift);
+  return q;
 }
 
-// A workgroup of four waves a (request, new token, query head); a wave takes every fourth key,
-// its lanes the head dims, with the online softmax recurrence; the four states are joined in LDS.
-template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void paged_simple_kernel(const PagedArgs a) {
-  constexpr int E = D / 64;
-  __shared__ float s_part[4][D + 2];
-  const int hq = blockIdx.x % a.Hq, t = blockIdx.x / a.Hq % a.max_new, r = blockIdx.x / a.Hq / a.max_new;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row0 = a.cu ? min(max(a.cu[r], 0), a.T) : r, row1 = a.cu ? min(max(a.cu[r + 1], row0), a.T) : r + 1;
-  if (t >= row1 - row0) return;
-  const int h = hq / (a.Hq / a.Hkv);
-  const int len = a.lens[r];
-  const long long cap = (long long)a.max_pages << a.page_shift;
-  const int end = (int)max(0ll, min(min((long long)len, cap), (long long)len - (row1 - row0) + t + 1));
-  float qv[E], acc[E];
-  const long long qrow = (long long)(row0 + t) * a.Hq + hq;
+__device__ const uint8_t g_zero_row[256] __attribute__((aligned(256))) = {};  // read in place of masked rows
+
+// A value that is the same in every lane, to scalar registers.
+__device__ __forceinline__ long long uniform(long long x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)x), up = __builtin_amdgcn_readfirstlane((int)(x >> 32));
+  return (long long)((unsigned long long)up << 32 | lo);
+}
+
+// XOR swizzle of the 16-byte chunks of an LDS row of RB bytes.
+template <int RB>
+__device__ __forceinline__ int row_swz(int r) {
+  if constexpr (RB == 256) return swz<128>(r);
+  else if constexpr (RB == 128) return swz<64>(r);
+  else return (r >> 2) & 3;
+}
+
+__device__ __forceinline__ bf16x8 from_e4m3(uint32_t lo, uint32_t hi, float scale) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+  const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// One wave a workgroup.  Per tile the arithmetic of the decode kernel over a contiguous cache:
+// S^T = K Q^T on the matrix cores (K rows with bits 2 and 3 of the row index swapped as the A
+// operand, a lane one query slot), lazy online softmax, O^T += V^T P^T with V^T from the
+// transpose reads of LDS.  Tiles are double buffered: the direct-to-LDS loads of tile i + 1,
+// every row at an address of its own (pages of any size), are in flight while tile i is computed.
+// 8-bit tiles become bf16 operands in registers, exactly: key rows under their scales, values as
+// they are, their scales (powers of two) going into the probabilities before those are rounded.
+template <int D, bool F8>
+__global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
+  constexpr int RB = F8 ? D : 2 * D;              // bytes a row
+  constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
+  constexpr int KT = 8192 / RB < 64 ? 8192 / RB : 64;  // keys a tile
+  constexpr int LOADS = KT / RPL, NS = KT / 32, NKK = D / 16, NDT = D / 32;
+  constexpr int TB = KT * RB;                     // bytes of a tile; its scales: a dword a key
+  __shared__ __attribute__((aligned(1024))) uint8_t sK[2][TB];
+  __shared__ __attribute__((aligned(1024))) uint8_t sV[2][TB];
+  __shared__ __attribute__((aligned(256))) uint32_t sKS[2][F8 ? 64 : 1];
+  __shared__ __attribute__((aligned(256))) uint32_t sVS[2][F8 ? 64 : 1];
+  const int lane = threadIdx.x, l32 = lane & 31, hi = lane >> 5;
+  const int w = blockIdx.x, G = a.Hq / a.Hkv;
+
+  // ---- this wave's share of the units ----
+  auto units = [&](int r) -> long long {  // of request r
+    if (r >= a.R) return 0;
+    const Request q = request(a, r);
+    const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
+    return (long long)a.Hkv * rounds * tiles;
+  };
+  auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    qv[e] = (float)a.q[qrow * D + lane * E + e] * a.scale;
-    acc[e] = 0.f;
+    for (int off = 1; off < 64; off <<= 1) {
+      const long long y = __shfl_up(v, off);
+      if (lane >= off) v += y;
+    }
+    return v;
+  };
+  const int per = (a.R + 63) / 64;  // requests a lane sums
+  long long mine = 0;
+  for (int j = 0; j < per; ++j) mine += units(lane * per + j);
+  const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
+  const long long share = max((long long)kMinShare, (total + kWorkers - 1) / kWorkers);
+  const long long u0 = share * w, u1 = min(total, u0 + share);
+  if (!a.by_group && lane == 0) a.split[w].parts = 0;
+  if (u0 >= u1) return;
+  // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
+  int r;
+  long long r_at;  // first unit of request r
+  {
+    const int l = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
+    r_at = __shfl(upto - mine, l);
+    r = l * per;
+    const long long v = lane < per ? units(r + lane) : 0, s = scan(v);
+    const int k = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
+    r_at += __shfl(s - v, k);
+    r += k;
   }
-  float m = -INFINITY, l = 0.f;
-  for (int p = wave; p < end; p += 4) {
-    const int page = a.table[(long long)r * a.max_pages + (p >> a.page_shift)];
-    if (page < 0 || page >= a.n_pages) continue;
-    const long long row = (((long long)page << a.page_shift) + (p & ((1 << a.page_shift) - 1))) * a.Hkv + h;
-    float kv[E], vv[E];
+  r = __builtin_amdgcn_readfirstlane(r);
+  r_at = uniform(r_at);
+
+  // ---- constants of the tile loop ----
+  const float sl2 = a.scale * kLog2e;
+  const int rs = a.Hkv * RB;  // bytes a token
+  const int page_mask = (1 << a.page_shift) - 1;
+  // Offsets in a tile.  The swizzle is an XOR of the chunk's number, so the steps over chunks are
+  // XORs as well; a step over rows that changes the swizzle (loads) is one of a constant.
+  const int load_row = lane / CPR, load_off = 16 * ((lane % CPR) ^ row_swz<RB>(load_row));
+  auto chunk = [&](int j) { return load_off ^ (16 * (row_swz<RB>(j * RPL) ^ row_swz<RB>(0))); };
+  const int krow = swap_bits23(l32), koff = krow * RB + 16 * (hi ^ row_swz<RB>(krow));
+  const int g16 = lane >> 4, li = lane & 15;
+  int voff[2];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const long long i = row * D + lane * E + e;
-      if constexpr (E4M3) {
-        kv[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)a.k)[i], 0) * ldexpf(1.f, a.ks[row] - 127);
-        vv[e] = __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)a.v)[i], 0) * ldexpf(1.f, a.vs[row] - 127);
+  for (int i = 0; i < 2; ++i) {
+    const int row = F8 ? 8 * hi + (li >> 1) : 8 * hi + 4 * i + (li >> 2);
+    const int byte = F8 ? 16 * (g16 & 1) + 8 * (li & 1) : 2 * (16 * (g16 & 1) + 4 * (li & 3));
+    voff[i] = row * RB + 16 * ((byte >> 4) ^ row_swz<RB>(row)) + (byte & 15);
+  }
+
+  for (long long u = u0; u < u1;) {
+    // ---- the group of unit u: request r, key head h, round of slots; its tiles [t0, t1) ----
+    Request q = request(a, r);
+    int tiles, rounds;
+    for (;;) {
+      rounds = (q.n * G + kSlots - 1) / kSlots;
+      tiles = max(1, (q.keys + KT - 1) / KT);
+      const long long end = r_at + (long long)a.Hkv * rounds * tiles;
+      if (u < end) break;
+      r_at = end;
+      q = request(a, ++r);
+    }
+    const long long in_r = u - r_at, grp = in_r / tiles;
+    const int t0 = (int)(in_r - grp * tiles), t1 = (int)min((long long)tiles, t0 + (u1 - u));
+    const int h = (int)(grp / rounds), slot0 = (int)(grp - (long long)h * rounds) * kSlots;
+    const int slots = min(kSlots, q.n * G - slot0);
+    const int n = slot0 + min(l32, slots - 1), t = n / G;  // this lane's slot
+    const long long qrow = (long long)(q.row0 + t) * a.Hq + h * G + (n - t * G);
+    const int qpos = q.first + t;
+
+    bf16x8 qreg[NKK];
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk) {
+      const int d = F8 ? 32 * (kk / 2) + 16 * hi + 8 * (kk & 1) : 16 * kk + 8 * hi;
+      const bf16x8 x = *(const bf16x8*)(a.q + qrow * D + d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qreg[kk][e] = l32 < slots ? x[e] : (bf16)0.f;
+    }
+
+    f32x16 oacc[NDT];
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f, m_eff = 0.f, thr = -INFINITY;
+    // slot of key row `lane` of tile i in the cache, or -1; the ids of 64 pages are at hand
+    const int* trow = a.table + (long long)r * a.max_pages;
+    int ids = -1, ids_at = -1;
+    auto slot_of = [&](int i) __attribute__((always_inline)) {
+      const int p = i * KT + lane, page = p >> a.page_shift, at = (i * KT >> a.page_shift) & ~63;
+      if (at != ids_at) {  // pages of a tile are 64 at most and aligned: of one such run
+        ids = at + lane < a.max_pages ? trow[at + lane] : -1;
+        ids_at = at;
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(ids));  // here, not at every tile's use of ids
+      }
+      const int id = __shfl(ids, page & 63);
+      const bool there = lane < KT && p < q.keys && id >= 0 && id < a.n_pages;
+      return there ? (id << a.page_shift) + (p & page_mask) : -1;
+    };
+    const uint8_t* kb = (const uint8_t*)a.k + h * RB;
+    const uint8_t* vb = (const uint8_t*)a.v + h * RB;
+    auto load_tile = [&](int s, int b) __attribute__((always_inline)) {  // into buffer b
+      if constexpr (F8) {
+        const long long i = (long long)max(s, 0) * a.Hkv + h;
+        dma_lds1_at(a.ks + i, lds_addr(sKS[b]));
+        dma_lds1_at(a.vs + i, lds_addr(sVS[b]));
+      }
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const int row = __shfl(s, j * RPL + load_row);
+        const long long off = (long long)row * rs + chunk(j);
+        dma_lds16_at(row >= 0 ? kb + off : g_zero_row + chunk(j), lds_addr(sK[b]) + j * 1024);
+        dma_lds16_at(row >= 0 ? vb + off : g_zero_row + chunk(j), lds_addr(sV[b]) + j * 1024);
+      }
+    };
+
+    int s_cur = slot_of(t0);
+    load_tile(s_cur, 0);
+
+#pragma unroll 1
+    for (int it = t0; it < t1; ++it) {
+      const int b = (it - t0) & 1;
+      const uint64_t present = __builtin_amdgcn_ballot_w64(s_cur >= 0);  // keys of the tile that exist
+      // the previous tile's LDS reads have all returned before its buffer is refilled
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (it + 1 < t1) {
+        s_cur = slot_of(it + 1);
+        load_tile(s_cur, b ^ 1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS + (F8 ? 2 : 0)) : "memory");  // tile it landed
       } else {
-        kv[e] = (float)((const bf16*)a.k)[i];
-        vv[e] = (float)((const bf16*)a.v)[i];
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+      const uint8_t* kt = sK[b];
+      uint8_t* vt = sV[b];
+      const int k0 = it * KT;
+      // keys that some row of the request does not see, or none does
+      const bool diagonal = k0 + KT - 1 > q.first;
+      const bool masked = diagonal || present != (KT == 64 ? ~0ull : (1ull << KT) - 1);
+      bool odd = false;  // a value that is not finite in a tile that some rows see only in part
+      if (diagonal && q.n > 1) {
+#pragma unroll
+        for (int i = 0; i < KT * RB / 1024; ++i) {
+          const u32x4 x = *(const u32x4*)(vt + i * 1024 + lane * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (F8) {
+              const uint32_t y = (x[e] & 0x7f7f7f7fu) + 0x01010101u;  // 0x7f becomes 0x80
+              odd |= (y & 0x80808080u) != 0;
+            } else {
+              odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+            }
+          }
+        }
+        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
+      }
+#pragma unroll
+      for (int sub = 0; sub < NS; ++sub) {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        if constexpr (F8) {
+          const float ksc = __uint_as_float(sKS[b][32 * sub + krow] << 23);
+#pragma unroll
+          for (int kk = 0; kk < NKK; kk += 2) {
+            const u32x4 x = *(const u32x4*)(kt + 32 * sub * RB + (koff ^ (16 * kk)));
+            s = mfma32(from_e4m3(x[0], x[1], ksc), qreg[kk], s);
+            s = mfma32(from_e4m3(x[2], x[3], ksc), qreg[kk + 1], s);
+          }
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < NKK; ++kk)
+            s = mfma32(*(const bf16x8*)(kt + 32 * sub * RB + (koff ^ (32 * kk))), qreg[kk], s);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], sl2, -m_eff);  // log2 units
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = 32 * sub + 16 * (i >> 3) + 8 * hi + (i & 7);
+            if (k0 + key > qpos || !(present >> key & 1)) s[i] = -INFINITY;
+          }
+        }
+        // lazy rescale: raise the running maximum only when a score exceeds it by kTau
+        float mx = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        const float mx2 = pair_max(mx);
+        if (__builtin_amdgcn_ballot_w64(mx2 > thr)) {
+          const float m_new = fmaxf(m_run, m_eff + mx2);
+          const float m_new_eff = (m_new == -INFINITY) ? 0.f : m_new;
+          const float alpha = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - m_new);
+          const float delta = m_new_eff - m_eff;
+          // (a slot that has seen no key keeps zero sums: 0 * alpha; NaN sums stay NaN)
+          l_run *= alpha;
+#pragma unroll
+          for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[dt][i] *= alpha;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] -= delta;
+          m_run = m_new;
+          m_eff = m_new_eff;
+          thr = (m_new == -INFINITY) ? -INFINITY : kTau;
+        }
+        // Probabilities; the denominator sums them as they are, the products take them rounded to
+        // bf16 (half a step each: o gains 2^-8 of the mean of |v| at most).
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) l_run += (s[i] + s[i + 1]) + (s[i + 2] + s[i + 3]);
+        if constexpr (F8) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t* sc = sVS[b] + 32 * sub + 16 * g + 8 * hi;
+            const u32x4 lo = *(const u32x4*)sc, up = *(const u32x4*)(sc + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)  // (0 stays 0 under any scale)
+              s[8 * g + e] = __builtin_ldexpf(s[8 * g + e], (int)(e < 4 ? lo[e & 3] : up[e & 3]) - 127);
+          }
+        }
+        bf16x8 pb[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          u32x4 pw;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) pw[j] = pack_bf16x2(s[8 * g + 2 * j], s[8 * g + 2 * j + 1]);
+          pb[g] = __builtin_bit_cast(bf16x8, pw);
+        }
+        uint8_t* vs = vt + 32 * sub * RB;
+        auto values = [&](int g, int dt) __attribute__((always_inline)) {  // 16 keys x 32 dims of V^T
+          const uint8_t* vg = vs + 16 * g * RB;
+          if constexpr (F8) {
+            typedef int i32x2_t __attribute__((ext_vector_type(2)));
+            const i32x2_t x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                (__attribute__((address_space(3))) i32x2_t*)((lds_void*)(vg + (voff[0] ^ (32 * dt)))));
+            return from_e4m3((uint32_t)x[0], (uint32_t)x[1], 1.f);
+          } else {
+            const bf16x4 lo = lds_read_tr16((const bf16*)(vg + (voff[0] ^ (64 * dt))));
+            const bf16x4 up = lds_read_tr16((const bf16*)(vg + (voff[1] ^ (64 * dt))));
+            return bf16x8{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
+          }
+        };
+        if (!odd) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) oacc[dt] = mfma32(values(g, dt), pb[g], oacc[dt]);
+        } else {
+          // 0 * inf is NaN in the products: token by token, the last first, the values past its
+          // position overwritten by zeros, and only its slots' sums kept
+          int zeros = 32;
+#pragma unroll 1
+          for (int tt = q.n - 1; tt >= 0; --tt) {
+            const int keep = min(max(q.first + tt + 1 - k0 - 32 * sub, 0), 32);
+            for (int row = keep; row < zeros; ++row)
+              if (lane < CPR) *(u32x4*)(vs + row * RB + 16 * lane) = u32x4{0, 0, 0, 0};
+            zeros = min(zeros, keep);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int dt = 0; dt < NDT; ++dt) {
+              f32x16 x;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = 0.f;
+              x = mfma32(values(0, dt), pb[0], x);
+              x = mfma32(values(1, dt), pb[1], x);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) oacc[dt][i] = t == tt ? oacc[dt][i] + x[i] : oacc[dt][i];
+            }
+          }
+        }
       }
     }
-    float s = 0.f;
+
+    // ---- the result, or this wave's part of it ----
+    const float l = pair_sum(l_run);
+    const bool whole = t0 == 0 && t1 == tiles;
+    if (l32 < slots) {
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16* out = a.o + qrow * D;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s = fmaf(qv[e], kv[e], s);
-    s = wave_sum(s);
-    if (s == -INFINITY) continue;  // weighs nothing
-    const float mn = s == s ? fmaxf(m, s) : INFINITY;  // a NaN makes everything after it NaN
-    const float alpha = m == -INFINITY ? 0.f : expf(m - mn), w = expf(s - mn);
-    l = l * alpha + w;
+        for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(w, vv[e], acc[e] * alpha);
-    m = mn;
+          for (int g = 0; g < 4; ++g) {
+            const f32x4 x{oacc[dt][4 * g], oacc[dt][4 * g + 1], oacc[dt][4 * g + 2], oacc[dt][4 * g + 3]};
+            *(u32x2*)(out + 32 * dt + 8 * g + 4 * hi) =
+                u32x2{pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv)};
+          }
+        if (!hi) a.lse[qrow] = l == 0.f ? -INFINITY : m_eff * kLn2 + logf(l);
+      } else {
+        const long long part = ((long long)2 * w + (u == u0 ? 0 : 1)) * a.M + l32;
+        float* acc = a.part_acc + part * D;
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *(f32x4*)(acc + 32 * dt + 8 * g + 4 * hi) =
+                f32x4{oacc[dt][4 * g], oacc[dt][4 * g + 1], oacc[dt][4 * g + 2], oacc[dt][4 * g + 3]};
+        if (!hi) *(f32x2*)(a.part_ml + 2 * part) = f32x2{m_run, l};
+      }
+    }
+    if (t0 == 0 && lane == 0 && (a.by_group || !whole)) {
+      const long long last = u + tiles - 1;  // the group's last unit
+      a.split[a.by_group ? (r * a.Hkv + h) * a.rounds + slot0 / kSlots : w] =
+          Split{q.row0, h, slot0, slots, 2 * w + (u == u0 ? 0 : 1), whole ? 0 : (int)(last / share) - w + 1};
+    }
+    u += t1 - t0;
+    // the buffers are refilled by the next group's first loads
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// Joins the parts of the groups that several waves share: a workgroup of 8 waves takes one query
+// slot of one entry.  The weights 2^(m - M) of the parts go to LDS; wave i sums every eighth part,
+// its loads independent of one another, and the eight sums are added in order.
+constexpr int kJoinWaves = 8;
+
+template <int D>
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const PagedArgs a) {
+  constexpr int E = D / 64;
+  __shared__ float s_w[kWorkers];
+  __shared__ float s_red[2][kJoinWaves];
+  __shared__ float s_part[kJoinWaves][D];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.Hq / a.Hkv, slot = blockIdx.y;
+  if (a.by_group) {  // an entry is there if its request has such a round
+    const int g = blockIdx.x / a.rounds, round = blockIdx.x - g * a.rounds;
+    if (request(a, g / a.Hkv).n * G <= round * kSlots) return;
+  }
+  const Split sp = a.split[blockIdx.x];
+  if (sp.parts == 0 || slot >= sp.slots) return;
+  auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i)) * a.M + slot; };
+  float mx = -INFINITY;
+  for (int i = tid; i < sp.parts; i += 64 * kJoinWaves) {
+    const float m = a.part_ml[2 * part(i)];
+    s_w[i] = m;
+    mx = fmaxf(mx, m);
   }
 #pragma unroll
-  for (int e = 0; e < E; ++e) s_part[wave][lane * E + e] = acc[e];
-  if (lane == 0) {
-    s_part[wave][D] = m;
-    s_part[wave][D + 1] = l;
+  for (int off = 32; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
+  if (lane == 0) s_red[0][wave] = mx;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinWaves; ++i) mx = fmaxf(mx, s_red[0][i]);
+  const float m_eff = mx == -INFINITY ? 0.f : mx;
+  float l = 0.f;
+  for (int i = tid; i < sp.parts; i += 64 * kJoinWaves) {
+    const float li = a.part_ml[2 * part(i) + 1], wt = li == 0.f ? 0.f : exp2f(s_w[i] - m_eff);
+    s_w[i] = wt;
+    l = fmaf(li, wt, l);
   }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
+  if (lane == 0) s_red[1][wave] = l;
+  __syncthreads();
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll 8
+  for (int i = wave; i < sp.parts; i += kJoinWaves) {
+    const float* x = a.part_acc + part(i) * D;
+    const float wt = s_w[i];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane + 64 * e], wt, acc[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_part[wave][lane + 64 * e] = acc[e];
   __syncthreads();
   if (wave != 0) return;
-  float mt = -INFINITY, lt = 0.f, ot[E] = {};
-  for (int w = 0; w < 4; ++w) mt = fmaxf(mt, s_part[w][D]);
-  for (int w = 0; w < 4; ++w) {
-    const float f = s_part[w][D] == -INFINITY ? 0.f : expf(s_part[w][D] - mt);
-    lt = fmaf(s_part[w][D + 1], f, lt);
+  l = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) ot[e] += f == 0.f ? 0.f : s_part[w][lane * E + e] * f;
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+  for (int i = 0; i < kJoinWaves; ++i) {
+    l += s_red[1][i];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += s_part[i][lane + 64 * e];
   }
+  const int n = sp.slot0 + slot, t = n / G;
+  const long long qrow = (long long)(sp.row0 + t) * a.Hq + sp.h * G + (n - t * G);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < E; ++e) a.o[qrow * D + lane * E + e] = (bf16)(mt == -INFINITY ? 0.f : ot[e] / lt);
-  if (lane == 0) a.lse[qrow] = mt == -INFINITY ? -INFINITY : mt + logf(lt);
+  for (int e = 0; e < E; ++e) a.o[qrow * D + lane + 64 * e] = (bf16)(acc[e] * inv);
+  if (lane == 0) a.lse[qrow] = l == 0.f ? -INFINITY : m_eff * kLn2 + logf(l);
 }
 
 }  // namespace
@@ -139,11 +554,17 @@ static int paged_check(const void* q, const void* k_pages, const void* v_pages, 
   return RA_OK;
 }
 
+// Query slots of a group at most, and the bytes of the partial states and entries of `waves` waves.
+static int paged_slots(int Hq, int Hkv, int max_new) { return std::min(kSlots, max_new * (Hq / Hkv)); }
+static size_t paged_bytes(int waves, int M, int D) {
+  return (size_t)waves * (2 * (size_t)M * (D + 2) * sizeof(float) + sizeof(Split));
+}
+
 extern "C" int paged_attn_workspace(int R, int Hq, int Hkv, int D, int max_new, size_t* bytes) {
   g_err.clear();
   if (!bytes) return set_err(RA_EINVAL, "null pointer argument");
   if (int e = paged_check_heads(R, Hq, Hkv, D, max_new)) return e;
-  *bytes = 0;
+  *bytes = paged_bytes(kWorkers, paged_slots(Hq, Hkv, max_new), D);
   return RA_OK;
 }
 
@@ -157,14 +578,33 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
                        n_pages, page_size, max_pages, max_new, kv_type);
   if (rc) return rc;
   if (int e = check_aligned({workspace})) return e;
-  PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, T, R,
-              Hq, Hkv, n_pages, 0, max_pages, max_new, 1.f / sqrtf((float)D)};
+  const bool f8 = kv_type == RA_KV_E4M3;
+  const int W = kWorkers, M = paged_slots(Hq, Hkv, max_new);
+  const int rounds = (int)(((long long)max_new * (Hq / Hkv) + kSlots - 1) / kSlots);
+  const size_t need = paged_bytes(kWorkers, M, D);
+  if (workspace && workspace_bytes < need)
+    return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+  CallResources res(stream);
+  if (!workspace) {
+    if ((rc = res.alloc(need))) return rc;
+    workspace = res.ws;
+  }
+  const long long groups = (long long)R * Hkv * rounds;
+  float* acc = (float*)workspace;
+  float* ml = acc + (size_t)W * 2 * M * D;
+  PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, acc, ml,
+              (Split*)(ml + (size_t)W * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
+              groups <= W, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
-  auto* kern = D == 128 ? (k_scales ? paged_simple_kernel<128, true> : paged_simple_kernel<128, false>)
-                        : (k_scales ? paged_simple_kernel<64, true> : paged_simple_kernel<64, false>);
+  auto* kern = D == 128 ? (f8 ? paged_partial_kernel<128, true> : paged_partial_kernel<128, false>)
+                        : (f8 ? paged_partial_kernel<64, true> : paged_partial_kernel<64, false>);
   RA_HIP(timed_launch(RA_KERNEL_DECODE, stream, [&] {
-    hipLaunchKernelGGL(kern, dim3((unsigned)R * max_new * Hq), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(kern, dim3(W), dim3(64), 0, stream, a);
     return hipGetLastError();
   }));
+  const dim3 grid(a.by_group ? (unsigned)groups : W, M);
+  if (D == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(64 * kJoinWaves), 0, stream, a);
+  else hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(64 * kJoinWaves), 0, stream, a);
+  RA_HIP(hipGetLastError());
   return RA_OK;
 }

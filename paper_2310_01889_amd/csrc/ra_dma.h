@@ -26,6 +26,14 @@ __device__ __forceinline__ void dma_lds4(const __amdgpu_buffer_rsrc_t& rsrc, uns
   asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(lds_addr), "v"(voff), "s"(rsrc)
                : "memory");
 }
+// As dma_lds16, each lane reading an address of its own; and one byte a lane, which lands
+// zero-extended in lane i's dword at byte 4 i.
+__device__ __forceinline__ void dma_lds16_at(const void* addr, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
+}
+__device__ __forceinline__ void dma_lds1_at(const void* addr, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
+}
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* base, int num_bytes) {
   return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, num_bytes, 0x00020000);
 }

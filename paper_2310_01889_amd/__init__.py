@@ -406,90 +406,87 @@ def llama_stack_train_step(x, layer_params, dz, z, dx, layer_grads, n_heads, n_h
           garr, len(layer_params), S, dm, int(n_heads), dff, int(n_hosts), int(causal), _stream(stream))
 
 
-def _here(*ts):
-    """The tensors must live on the current GPU: its stream runs the call."""
-    d = torch.cuda.current_device()
-    for t in ts:
-        if t is not None and t.get_device() != d:
-            raise ValueError("tensors must be on the current GPU (cuda:%d), got %s" % (d, t.device))
+# The calls of a decode step take a few microseconds on the GPU, so their checks are kept short: one
+# pass over a tensor in `_arg` (about half the host time of `_ptr`), the raw stream handle.
+_BF16, _F32, _I32, _U8, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
 
 
-def _sized(t, name, *shape):
-    if tuple(t.shape) != shape:
-        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+def _arg(t, name, dtype, dev, shape=None):
+    """Address of a dense tensor on the current GPU `dev` of this type and shape; None for None."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
+    _ptr(t, dtype, name)
+    if t.get_device() != dev:
+        raise ValueError("%s must be on the current GPU (cuda:%d), got %s" % (name, dev, t.device))
+    raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def _rows(t, name, T, H, D, dev):
+    """Address and row stride of a bf16 [T, H, D] tensor whose rows are dense."""
+    if t.shape != (T, H, D):
+        raise ValueError("%s must be %s, got %s" % (name, [T, H, D], list(t.shape)))
+    row, head, elem = t.stride()
+    if (D > 1 and elem != 1) or (H > 1 and head != D):
+        raise ValueError("the heads of a row of %s must be contiguous" % name)
+    if t.dtype is not _BF16 or t.get_device() != dev:
+        _arg(t[:1].contiguous(), name, _BF16, dev)  # says what is wrong
+    return t.data_ptr(), row if T > 1 else H * D
+
+
+def _cache(k_pages, v_pages, k_scales, v_scales, dev):
+    """Addresses of a cache's tensors, its kv_type and its shape."""
+    shape, dt = k_pages.shape, k_pages.dtype
+    if len(shape) != 4:
+        raise ValueError("expected a [n_pages, page_size, Hkv, D] cache")
+    if dt is not _BF16 and dt is not _E4M3:
+        raise TypeError("k_pages must be torch.bfloat16 or torch.float8_e4m3fn, got %s" % dt)
+    kp, vp = _arg(k_pages, "k_pages", dt, dev), _arg(v_pages, "v_pages", dt, dev, shape)
+    if dt is _BF16 and k_scales is None and v_scales is None:
+        return kp, vp, None, None, 0, shape
+    return (kp, vp, _arg(k_scales, "k_scales", _U8, dev, shape[:3]), _arg(v_scales, "v_scales", _U8, dev, shape[:3]),
+            0 if dt is _BF16 else 1, shape)
+
+
+def _current(stream):
+    """The current GPU and the handle of the stream a call runs on."""
+    dev = torch.cuda.current_device()
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def paged_plan(lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts, page_size,
                n_pages, stream=None):
     """int32 tensors: lens, n_new, new_lens [R], free_pages [n_free], free_head [1] or None,
     block_table [R, max_pages], cu_rows [R + 1], slots, positions [T], counts [4]."""
-    R, max_pages = (int(x) for x in block_table.shape)
-    T, i32 = int(slots.shape[0]), torch.int32
-    _here(lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts)
-    for t, name, n in ((lens, "lens", R), (n_new, "n_new", R), (cu_rows, "cu_rows", R + 1), (new_lens, "new_lens", R),
-                       (slots, "slots", T), (positions, "positions", T), (counts, "counts", 4)):
-        _sized(t, name, n)
-    _call("paged_plan", _ptr(lens, i32, "lens"), _ptr(n_new, i32, "n_new"), _ptr(free_pages, i32, "free_pages"),
-          _ptr(free_head, i32, "free_head"), _ptr(block_table, i32, "block_table"), _ptr(cu_rows, i32, "cu_rows"),
-          _ptr(new_lens, i32, "new_lens"), _ptr(slots, i32, "slots"), _ptr(positions, i32, "positions"),
-          _ptr(counts, i32, "counts"), R, int(page_size), max_pages, int(n_pages), int(free_pages.numel()), T,
-          _stream(stream))
-
-
-KV_BF16, KV_E4M3 = 0, 1
-
-
-def _cache(k_pages, v_pages, k_scales, v_scales):
-    """Pointers of a cache's tensors, its kv_type and its shape."""
-    if k_pages.dim() != 4:
-        raise ValueError("expected a [n_pages, page_size, Hkv, D] cache")
-    shape = tuple(int(x) for x in k_pages.shape)
-    _sized(v_pages, "v_pages", *shape)
-    dt = k_pages.dtype
-    if dt not in (torch.bfloat16, torch.float8_e4m3fn):
-        raise TypeError("k_pages must be torch.bfloat16 or torch.float8_e4m3fn, got %s" % dt)
-    for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales")):
-        if t is not None:
-            _sized(t, name, *shape[:3])
-    u8 = torch.uint8
-    return ((_ptr(k_pages, dt, "k_pages"), _ptr(v_pages, dt, "v_pages"), _ptr(k_scales, u8, "k_scales"),
-             _ptr(v_scales, u8, "v_scales")), KV_BF16 if dt == torch.bfloat16 else KV_E4M3, shape)
-
-
-def _rows(t, name, T, H, D):
-    """Pointer and row stride of a bf16 [T, H, D] tensor whose rows are dense."""
-    _sized(t, name, T, H, D)
-    if t.dtype != torch.bfloat16:
-        raise TypeError("%s must be torch.bfloat16, got %s" % (name, t.dtype))
-    if not t.is_cuda:
-        raise ValueError("%s must be a GPU tensor" % name)
-    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
-        raise ValueError("the heads of a row of %s must be contiguous" % name)
-    return ctypes.c_void_p(t.data_ptr()), int(t.stride(0)) if T > 1 else H * D
+    R, max_pages = block_table.shape
+    T, (dev, st) = len(slots), _current(stream)
+    _call("paged_plan", _arg(lens, "lens", _I32, dev, (R,)), _arg(n_new, "n_new", _I32, dev, (R,)),
+          _arg(free_pages, "free_pages", _I32, dev, (len(free_pages),)), _arg(free_head, "free_head", _I32, dev, (1,)),
+          _arg(block_table, "block_table", _I32, dev), _arg(cu_rows, "cu_rows", _I32, dev, (R + 1,)),
+          _arg(new_lens, "new_lens", _I32, dev, (R,)), _arg(slots, "slots", _I32, dev, (T,)),
+          _arg(positions, "positions", _I32, dev, (T,)), _arg(counts, "counts", _I32, dev, (4,)), R, page_size,
+          max_pages, n_pages, len(free_pages), T, st)
 
 
 def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=None, v_scales=None, rotate=True,
                  stream=None):
     """q [T, Hq, D] (or None, with q_out), k, v [T, Hkv, D]: rows may be strided."""
-    T = int(slots.shape[0])
-    ptrs, kind, (n_pages, page_size, Hkv, D) = _cache(k_pages, v_pages, k_scales, v_scales)
-    _here(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales, v_scales)
-    Hq = 0 if q is None else int(q.shape[1])
-    qp, qs = (None, 0) if q is None else _rows(q, "q", T, Hq, D)
-    kp, ks = _rows(k, "k", T, Hkv, D)
-    vp, vs = _rows(v, "v", T, Hkv, D)
-    if q_out is not None:
-        _sized(q_out, "q_out", T, Hq, D)
-    _sized(positions, "positions", T)
-    _call("paged_append", qp, kp, vp, _ptr(q_out, torch.bfloat16, "q_out"), *ptrs, _ptr(slots, torch.int32, "slots"),
-          _ptr(positions, torch.int32, "positions"), T, Hq, Hkv, D, qs, ks, vs, n_pages, page_size, kind,
-          int(bool(rotate)), _stream(stream))
+    T, (dev, st) = len(slots), _current(stream)
+    kp, vp, ks, vs, kind, (n_pages, page_size, Hkv, D) = _cache(k_pages, v_pages, k_scales, v_scales, dev)
+    Hq = 0 if q is None else q.shape[1]
+    q_at, q_row = (None, 0) if q is None else _rows(q, "q", T, Hq, D, dev)
+    k_at, k_row = _rows(k, "k", T, Hkv, D, dev)
+    v_at, v_row = _rows(v, "v", T, Hkv, D, dev)
+    _call("paged_append", q_at, k_at, v_at, _arg(q_out, "q_out", _BF16, dev, (T, Hq, D)), kp, vp, ks, vs,
+          _arg(slots, "slots", _I32, dev, (T,)), _arg(positions, "positions", _I32, dev, (T,)), T, Hq, Hkv, D, q_row,
+          k_row, v_row, n_pages, page_size, kind, 1 if rotate else 0, st)
 
 
 def paged_attn_workspace(R, Hq, Hkv, D, max_new):
     """Bytes of workspace a paged_attn_decode of this shape needs."""
     n = ctypes.c_size_t(0)
-    _call("paged_attn_workspace", int(R), int(Hq), int(Hkv), int(D), int(max_new), ctypes.byref(n))
+    _call("paged_attn_workspace", R, Hq, Hkv, D, max_new, ctypes.addressof(n))
     return n.value
 
 
@@ -497,51 +494,34 @@ def paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, m
                       workspace=None, stream=None):
     """q, o [T, Hq, D], lse [T, Hq]; cu_rows None: row r is the one new token of request r.
     workspace: a contiguous GPU tensor of paged_attn_workspace bytes, or None."""
-    if q.dim() != 3:
-        raise ValueError("expected a [T, Hq, D] tensor")
-    T, Hq, D = (int(x) for x in q.shape)
-    ptrs, kind, (n_pages, page_size, Hkv, Dc) = _cache(k_pages, v_pages, k_scales, v_scales)
+    T, Hq, D = q.shape
+    R, max_pages = block_table.shape
+    dev, st = _current(stream)
+    kp, vp, ks, vs, kind, (n_pages, page_size, Hkv, Dc) = _cache(k_pages, v_pages, k_scales, v_scales, dev)
     if Dc != D:
         raise ValueError("head dim %d of q, %d of the cache" % (D, Dc))
-    R, max_pages = (int(x) for x in block_table.shape)
-    _here(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, k_scales, v_scales, workspace)
-    _sized(o, "o", T, Hq, D)
-    _sized(lse, "lse", T, Hq)
-    _sized(lens, "lens", R)
-    if cu_rows is not None:
-        _sized(cu_rows, "cu_rows", R + 1)
-    i32, bf = torch.int32, torch.bfloat16
-    _call("paged_attn_decode", _ptr(q, bf, "q"), *ptrs, _ptr(block_table, i32, "block_table"), _ptr(lens, i32, "lens"),
-          _ptr(cu_rows, i32, "cu_rows"), _ptr(o, bf, "o"), _ptr(lse, torch.float32, "lse"),
-          _ptr(workspace, None, "workspace"), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-          T, R, Hq, Hkv, D, n_pages, page_size, max_pages, int(max_new), kind, _stream(stream))
+    ws, ws_bytes = None, 0
+    if workspace is not None:
+        ws, ws_bytes = _arg(workspace, "workspace", workspace.dtype, dev), workspace.numel() * workspace.element_size()
+    _call("paged_attn_decode", _arg(q, "q", _BF16, dev), kp, vp, ks, vs, _arg(block_table, "block_table", _I32, dev),
+          _arg(lens, "lens", _I32, dev, (R,)), _arg(cu_rows, "cu_rows", _I32, dev, (R + 1,)),
+          _arg(o, "o", _BF16, dev, (T, Hq, D)), _arg(lse, "lse", _F32, dev, (T, Hq)), ws, ws_bytes, T, R, Hq, Hkv, D,
+          n_pages, page_size, max_pages, max_new, kind, st)
 
 
 def mx4_pack(w, w4, scales, stream=None):
-    K, N = (int(s) for s in w.shape)
-    _here(w, w4, scales)
-    _mx_sized(w4, scales, K, N)
-    _call("mx4_pack", _ptr(w, torch.bfloat16, "w"), _ptr(w4, torch.uint8, "w4"), _ptr(scales, torch.uint8, "scales"),
-          K, N, _stream(stream))
-
-
-def _mx_sized(w4, scales, K, N):
+    (K, N), (dev, st) = w.shape, _current(stream)
     nb, kb = -(-N // 16), -(-K // 128)
-    _sized(w4, "w4", nb, kb, 64, 16)
-    _sized(scales, "scales", nb, kb, 16, 4)
+    _call("mx4_pack", _arg(w, "w", _BF16, dev), _arg(w4, "w4", _U8, dev, (nb, kb, 64, 16)),
+          _arg(scales, "scales", _U8, dev, (nb, kb, 16, 4)), K, N, st)
 
 
 def mx4_linear(x, w4, scales, residual, y, stream=None):
-    T, K = (int(s) for s in x.shape)
-    N = int(y.shape[1])
-    _here(x, w4, scales, residual, y)
-    _mx_sized(w4, scales, K, N)
-    _sized(y, "y", T, N)
-    if residual is not None:
-        _sized(residual, "residual", T, N)
-    bf, u8 = torch.bfloat16, torch.uint8
-    _call("mx4_linear", _ptr(x, bf, "x"), _ptr(w4, u8, "w4"), _ptr(scales, u8, "scales"),
-          _ptr(residual, bf, "residual"), _ptr(y, bf, "y"), T, K, N, _stream(stream))
+    (T, K), N, (dev, st) = x.shape, y.shape[1], _current(stream)
+    nb, kb = -(-N // 16), -(-K // 128)
+    _call("mx4_linear", _arg(x, "x", _BF16, dev), _arg(w4, "w4", _U8, dev, (nb, kb, 64, 16)),
+          _arg(scales, "scales", _U8, dev, (nb, kb, 16, 4)), _arg(residual, "residual", _BF16, dev, (T, N)),
+          _arg(y, "y", _BF16, dev, (T, N)), T, K, N, st)
 
 
 # ----------------------------------------------------------------------------------

@@ -63,34 +63,76 @@ struct MxArgs {
   int T, K, N, kb;
 };
 
-__device__ __forceinline__ float mx_scale(uint8_t b) { return b == 255 ? NAN : ldexpf(1.f, (int)b - 127); }
-__device__ __forceinline__ float e2m1(uint32_t c) {
-  const uint32_t m = c & 7;
-  const float v = m < 2 ? 0.5f * m : (1.f + 0.5f * (m & 1)) * (float)(1u << (m >> 1)) * 0.5f;
-  return c & 8 ? -v : v;
+// Eight codes (one dword) as a bf16 operand, exactly.  A scale byte of 255 makes an infinite scale,
+// under which the conversion gives NaN for every code (checked on the device).
+__device__ __forceinline__ bf16x8 from_e2m1(uint32_t codes, float scale) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+  const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A workgroup a block of 16 outputs and a row: 16 threads an output, each a share of the groups.
-__global__ __launch_bounds__(256) void mx4_simple_kernel(const MxArgs a) {
-  __shared__ float s_sum[16][17];
-  const int i = blockIdx.x, t = blockIdx.y, r = threadIdx.x % 16, part = threadIdx.x / 16;
-  float acc = 0.f;
-  for (int g = part; g < a.K / 32; g += 16) {
-    const long long block = (long long)i * a.kb + g / 4;
-    const float s = mx_scale(a.scales[(block * 16 + r) * 4 + g % 4]);
-    for (int c = 0; c < 4; ++c) {
-      const uint32_t word = *(const uint32_t*)(a.w4 + (block * 64 + c * 16 + r) * 16 + 4 * (g % 4));
-      const bf16* xr = a.x + (long long)t * a.K + 32 * g + 8 * c;
-      for (int j = 0; j < 8; ++j) acc = fmaf((float)xr[j], e2m1(word >> (4 * j) & 15) * s, acc);
+// A workgroup of 8 waves takes a block of 16 outputs for NT tiles of 16 rows; its waves take turns
+// of U weight blocks along the inputs, their sums are added in wave order through LDS.  Every
+// weight is read once a launch and becomes a bf16 operand once for all NT tiles; x comes from L2.
+constexpr int kMxWaves = 8;
+
+template <int NT, int U>
+__global__ __launch_bounds__(64 * kMxWaves) void mx4_linear_kernel(const MxArgs a) {
+  __shared__ f32x4 s_sum[kMxWaves][NT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, c = lane >> 4;
+  const int i = blockIdx.x, t0 = blockIdx.y * NT * 16;
+  const uint8_t* w4 = a.w4 + (long long)i * a.kb * 1024 + lane * 16;
+  const uint8_t* sc = a.scales + (long long)i * a.kb * 64 + l16 * 4;
+  f32x4 acc[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int b0 = wave * U; b0 < a.kb; b0 += kMxWaves * U) {
+    u32x4 w[U];
+    uint32_t e[U];
+    bf16x8 x[U][4][NT];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int b = min(b0 + u, a.kb - 1);
+      w[u] = *(const u32x4*)(w4 + (long long)b * 1024);
+      e[u] = *(const uint32_t*)(sc + (long long)b * 64);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          // (places past the ends read others' elements: for rows that are not stored, or unused)
+          const int k = min(128 * (b0 + u) + 32 * s, a.K - 32) + 8 * c, t = min(t0 + 16 * n + l16, a.T - 1);
+          x[u][s][n] = *(const bf16x8*)(a.x + (long long)t * a.K + k);
+        }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        if (128 * (b0 + u) + 32 * s >= a.K) break;
+        const bf16x8 wv = from_e2m1(w[u][s], __uint_as_float((e[u] >> (8 * s) & 255u) << 23));
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[n] = mfma16(wv, x[u][s][n], acc[n]);
+      }
   }
-  s_sum[part][r] = acc;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) s_sum[wave][n][lane] = acc[n];
   __syncthreads();
-  const int n = 16 * i + r;
-  if (part != 0 || n >= a.N) return;
-  for (int p = 1; p < 16; ++p) acc += s_sum[p][r];
-  const long long at = (long long)t * a.N + n;
-  a.y[at] = (bf16)(acc + (a.residual ? (float)a.residual[at] : 0.f));
+  if (wave >= NT) return;
+  f32x4 y = s_sum[0][wave][lane];
+#pragma unroll
+  for (int v = 1; v < kMxWaves; ++v) y += s_sum[v][wave][lane];
+  const int t = t0 + 16 * wave + l16, n0 = 16 * i + 4 * c;
+  if (t >= a.T) return;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const long long at = (long long)t * a.N + n0 + j;
+    if (n0 + j < a.N) a.y[at] = (bf16)(y[j] + (a.residual ? (float)a.residual[at] : 0.f));
+  }
 }
 
 int check_mx(int K, int N) {
@@ -127,7 +169,14 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
   if (T > kMxMaxT) return set_err(RA_EUNSUPPORTED, "T=%d exceeds %d rows", T, kMxMaxT);
   MxArgs a{(const bf16*)x, (const uint8_t*)w4, scales, (const bf16*)residual, (bf16*)y, T, d_in, d_out,
            (d_in + 127) / 128};
-  hipLaunchKernelGGL(mx4_simple_kernel, dim3((d_out + 15) / 16, T), dim3(256), 0, stream, a);
+  const int tiles = (T + 15) / 16;
+  auto run = [&](auto kernel, int nt) {
+    hipLaunchKernelGGL(kernel, dim3((d_out + 15) / 16, (tiles + nt - 1) / nt), dim3(64 * kMxWaves), 0, stream, a);
+  };
+  if (tiles == 1) run(mx4_linear_kernel<1, 4>, 1);
+  else if (tiles == 2) run(mx4_linear_kernel<2, 2>, 2);
+  else if (tiles == 3) run(mx4_linear_kernel<3, 2>, 3);
+  else run(mx4_linear_kernel<4, 2>, 4);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

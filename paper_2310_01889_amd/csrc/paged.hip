@@ -16,9 +16,8 @@ namespace ra {
 namespace {
 
 // ---- plan ----------------------------------------------------------------------------------
-constexpr int kPlanMaxR = kMaxRequests;  // their two prefix sums stay in LDS
 constexpr int kPlanThreads = 256;
-constexpr int kPlanRows = 4;     // rows a thread
+constexpr int kPlanRows = 4;  // rows a thread
 
 struct PlanArgs {
   const int *lens, *n_new, *free_pages, *free_head;
@@ -26,36 +25,41 @@ struct PlanArgs {
   int R, page_shift, max_pages, n_pages, n_free, T;
 };
 
-// Exclusive prefix sum over the workgroup's threads; *total is the sum of all.
-__device__ __forceinline__ long long block_scan(long long v, long long* total, long long* s_wave) {
+// Exclusive prefix sums of two values over the workgroup's threads, and the sums of all.
+struct Scan2 {
+  long long a, b, all_a, all_b;
+};
+__device__ __forceinline__ Scan2 block_scan(long long a, long long b, long long (*s_wave)[2]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  long long x = v;
+  long long x = a, y = b;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
-    const long long y = __shfl_up(x, off);
-    if (lane >= off) x += y;
+    const long long u = __shfl_up(x, off), v = __shfl_up(y, off);
+    if (lane >= off) x += u, y += v;
   }
   __syncthreads();  // an earlier scan's sums have been read
-  if (lane == 63) s_wave[wave] = x;
+  if (lane == 63) s_wave[wave][0] = x, s_wave[wave][1] = y;
   __syncthreads();
-  long long before = 0, all = 0;
+  Scan2 r{x - a, y - b, 0, 0};
 #pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) before += s_wave[w];
-    all += s_wave[w];
+    if (w < wave) r.a += s_wave[w][0], r.b += s_wave[w][1];
+    r.all_a += s_wave[w][0], r.all_b += s_wave[w][1];
   }
-  *total = all;
-  return before + x - v;
+  return r;
 }
 
 // Every workgroup forms the prefix sums of all requests' rows and pages (R is small and the
-// lengths stay in L2), then fills its share of the rows and of the requests' table entries: one
-// launch, no order between workgroups.  A new page's id is free_pages[head + its number in
-// request order], so nothing here depends on what another workgroup writes.
+// lengths stay in L2), then fills its share of the rows: one launch, no order between workgroups.
+// A new page's id is free_pages[head + its number in request order], so nothing here depends on
+// what another workgroup writes; its table entry is written by the row that opens it (a page is
+// only taken for a token).  Bound by latency: a handful of dependent loads and barriers.
 __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PlanArgs a) {
-  __shared__ int s_cu[kPlanMaxR + 1];    // first row of each request
-  __shared__ int s_page[kPlanMaxR + 1];  // number of its first new page (at most n_free)
-  __shared__ long long s_wave[kPlanThreads / 64];
+  extern __shared__ int s_req[];
+  int* s_cu = s_req;                   // [R + 1] first row of each request
+  int* s_page = s_req + a.R + 1;       // [R] number of its first new page (at most n_free)
+  int* s_len = s_page + a.R;           // [R] tokens it has in the cache
+  __shared__ long long s_wave[kPlanThreads / 64][2];
   const int tid = threadIdx.x;
   const int per = (a.R + kPlanThreads - 1) / kPlanThreads;
   const int r0 = min(a.R, tid * per), r1 = min(a.R, r0 + per);
@@ -63,63 +67,60 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PlanArgs
   const long long cap = (long long)a.max_pages << a.page_shift;
   int flags = 0;
   const int head_in = a.free_head ? *a.free_head : 0;
-  if (head_in < 0) flags |= RA_PLAN_BAD_INPUT;
-  const int head = min(max(head_in, 0), a.n_free);
-
-  // rows: a request takes no more of them than T holds
-  long long sum = 0, all_rows, total;
-  for (int r = r0; r < r1; ++r) {
-    const int n = a.n_new[r];
-    if (n < 0) flags |= RA_PLAN_BAD_INPUT;
-    sum += max(n, 0);
-  }
-  long long at = block_scan(sum, &all_rows, s_wave);
-  for (int r = r0; r < r1; ++r) {
-    s_cu[r] = (int)min(at, (long long)a.T);
-    at += max(a.n_new[r], 0);
-  }
-  if (tid == 0) s_cu[a.R] = (int)min(all_rows, (long long)a.T);
-  if (all_rows > a.T) flags |= RA_PLAN_ROWS;
-  __syncthreads();
 
   auto held = [&](long long tokens) { return (int)((min(tokens, cap) + P - 1) >> a.page_shift); };
-  sum = 0;
+  long long rows_sum = 0, page_sum = 0;
   for (int r = r0; r < r1; ++r) {
-    const int len = a.lens[r];
-    if (len < 0) flags |= RA_PLAN_BAD_INPUT;
-    const long long before = max(len, 0), after = before + s_cu[r + 1] - s_cu[r];
-    if (after > cap) flags |= RA_PLAN_CAPACITY;
-    sum += held(after) - held(before);
+    const int n = a.n_new[r], len = a.lens[r];
+    if (n < 0 || len < 0) flags |= RA_PLAN_BAD_INPUT;
+    s_cu[r] = max(n, 0);  // its number of rows, for now
+    s_len[r] = max(len, 0);
+    rows_sum += max(n, 0);
+    page_sum += held((long long)max(len, 0) + max(n, 0)) - held(max(len, 0));
+    if ((long long)max(len, 0) + max(n, 0) > cap) flags |= RA_PLAN_CAPACITY;
   }
-  at = block_scan(sum, &total, s_wave);
+  Scan2 at = block_scan(rows_sum, page_sum, s_wave);
+  const bool clipped = at.all_a > a.T;
+  if (clipped) {  // a request takes no more rows than T holds, and pages for those alone
+    flags = RA_PLAN_ROWS | (flags & RA_PLAN_BAD_INPUT);
+    long long row = at.a;
+    page_sum = 0;
+    for (int r = r0; r < r1; ++r) {
+      const int n = (int)min((long long)s_cu[r], max(0ll, a.T - row));
+      row += s_cu[r];
+      s_cu[r] = n;
+      const long long before = s_len[r], after = before + n;
+      page_sum += held(after) - held(before);
+      if (after > cap) flags |= RA_PLAN_CAPACITY;
+    }
+    const long long first = min(at.a, (long long)a.T);
+    at = block_scan(0, page_sum, s_wave);
+    at.a = first;
+    at.all_a = a.T;
+  }
+  long long row = at.a, page = at.b;
   for (int r = r0; r < r1; ++r) {
-    s_page[r] = (int)min(at, (long long)a.n_free);
-    const long long before = max(a.lens[r], 0), after = before + s_cu[r + 1] - s_cu[r];
-    at += held(after) - held(before);
+    const int n = s_cu[r];
+    s_cu[r] = (int)row;
+    s_page[r] = (int)min(page, (long long)a.n_free);
+    row += n;
+    page += held((long long)s_len[r] + n) - held(s_len[r]);
   }
+  const int rows = (int)at.all_a;
+  if (tid == 0) s_cu[a.R] = rows;
+  if (head_in < 0) flags |= RA_PLAN_BAD_INPUT;
+  const int head = min(max(head_in, 0), a.n_free);
   const long long left = a.n_free - head;
-  if (total > left) flags |= RA_PLAN_PAGES;
+  if (at.all_b > left) flags |= RA_PLAN_PAGES;
   __syncthreads();
 
-  auto fresh_page = [&](int r, int nth) {  // id of the nth new page of request r, or -1
-    const long long i = (long long)head + s_page[r] + nth;
-    const int id = i < a.n_free ? a.free_pages[i] : -1;
-    return id >= 0 && id < a.n_pages ? id : -1;
-  };
-
-  // table entries, offsets and lengths of this workgroup's requests
-  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
-    const long long before = max(a.lens[r], 0), after = before + s_cu[r + 1] - s_cu[r];
-    const int h0 = held(before), h1 = held(after);
-    for (int j = h0 + tid; j < h1; j += kPlanThreads) a.table[(long long)r * a.max_pages + j] = fresh_page(r, j - h0);
-    if (tid == 0) {
-      a.cu[r] = s_cu[r];
-      a.new_lens[r] = (int)min(after, 0x7fffffffll);
-    }
+  // this workgroup's share of the requests' offsets and lengths
+  for (int r = blockIdx.x * kPlanThreads + tid; r < a.R; r += gridDim.x * kPlanThreads) {
+    a.cu[r] = s_cu[r];
+    a.new_lens[r] = (int)min((long long)s_len[r] + s_cu[r + 1] - s_cu[r], 0x7fffffffll);
   }
 
-  // slots and positions of its rows
-  const int rows = s_cu[a.R];
+  // slots and positions of its rows, and the entries of the pages that they open
   const long long i0 = ((long long)blockIdx.x * kPlanThreads + tid) * kPlanRows;
   if (i0 < a.T) {
     int lo = 0, hi = a.R - 1;  // the last request that starts at or before row i0
@@ -134,11 +135,20 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PlanArgs
       int slot = -1, pos = -1;
       if (i < rows) {
         while (s_cu[r + 1] <= i) ++r;
-        const long long before = max(a.lens[r], 0), p = before + i - s_cu[r];
+        const long long before = s_len[r], p = before + i - s_cu[r];
         pos = (int)min(p, 0x7fffffffll);
         if (p < cap) {
           const int j = (int)(p >> a.page_shift), h0 = held(before);
-          const int id = j < h0 ? a.table[(long long)r * a.max_pages + j] : fresh_page(r, j - h0);
+          int* entry = a.table + (long long)r * a.max_pages + j;
+          int id;
+          if (j < h0) {
+            id = *entry;
+          } else {
+            const long long k = (long long)head + s_page[r] + (j - h0);
+            id = k < a.n_free ? a.free_pages[k] : -1;
+            if (id < 0 || id >= a.n_pages) id = -1;
+            if ((p & (P - 1)) == 0) *entry = id;
+          }
           if (id >= 0 && id < a.n_pages) slot = (id << a.page_shift) + (int)(p & (P - 1));
         }
       }
@@ -155,7 +165,7 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(const PlanArgs
     __syncthreads();
     if (tid == 0) {
       for (int w = 1; w < kPlanThreads / 64; ++w) flags |= s_flags[w];
-      const int took = (int)min(total, left);
+      const int took = (int)min(at.all_b, left);
       a.cu[a.R] = rows;
       a.counts[0] = rows;
       a.counts[1] = took;
@@ -324,13 +334,13 @@ extern "C" int paged_plan(const int* lens, const int* n_new, const int* free_pag
   if (R <= 0 || max_pages <= 0 || n_free <= 0 || T <= 0)
     return set_err(RA_EINVAL, "sizes must be positive (R=%d max_pages=%d n_free=%d T=%d)", R, max_pages, n_free, T);
   if (int e = check_pages(page_size, n_pages, 1, 1)) return e;
-  if (R > kPlanMaxR) return set_err(RA_EUNSUPPORTED, "R=%d exceeds %d requests", R, kPlanMaxR);
+  if (R > kMaxRequests) return set_err(RA_EUNSUPPORTED, "R=%d exceeds %d requests", R, kMaxRequests);
   PlanArgs a{lens, n_new, free_pages, free_head, block_table, cu_rows, new_lens, slots, positions, counts, R, 0,
              max_pages, n_pages, n_free, T};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   const int per = kPlanThreads * kPlanRows;
   const unsigned grid = (unsigned)(((long long)T + per - 1) / per);
-  hipLaunchKernelGGL(paged_plan_kernel, dim3(grid), dim3(kPlanThreads), 0, stream, a);
+  hipLaunchKernelGGL(paged_plan_kernel, dim3(grid), dim3(kPlanThreads), (3 * R + 1) * sizeof(int), stream, a);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

@@ -89,12 +89,17 @@ def test_mx4_refusals(lib):
     assert b"512" in lib.ring_attn_last_error()
 
 
-def test_binding_checks_shapes_before_calling():
-    with pytest.raises(ValueError):
-        ra._sized(torch.zeros(3), "x", 4)
-    with pytest.raises(ValueError):
-        ra._cache(torch.zeros(2, 4, 8), torch.zeros(2, 4, 8), None, None)
-    with pytest.raises(TypeError):
-        ra._cache(torch.zeros(2, 4, 1, 64), torch.zeros(2, 4, 1, 64), None, None)
+def test_binding_checks_tensors_before_calling():
+    bf = torch.bfloat16
     with pytest.raises(ValueError):  # not on the GPU
-        ra._rows(torch.zeros(2, 1, 64, dtype=torch.bfloat16), "q", 2, 1, 64)
+        ra._arg(torch.zeros(3, dtype=bf), "x", bf, 0, (3,))
+    with pytest.raises(ValueError):
+        ra._cache(torch.zeros(2, 4, 8), torch.zeros(2, 4, 8), None, None, 0)
+    with pytest.raises(TypeError):
+        ra._cache(torch.zeros(2, 4, 1, 64), torch.zeros(2, 4, 1, 64), None, None, 0)
+    with pytest.raises(ValueError):
+        ra._rows(torch.zeros(2, 1, 64, dtype=bf), "q", 2, 1, 64, 0)
+    with pytest.raises(ValueError):
+        ra._rows(torch.zeros(2, 1, 64, dtype=bf), "q", 3, 1, 64, 0)
+    with pytest.raises(ValueError):
+        ra._rows(torch.zeros(2, 64, 2, dtype=bf).transpose(1, 2), "q", 2, 2, 64, 0)

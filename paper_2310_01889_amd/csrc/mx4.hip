@@ -7,6 +7,7 @@
 #include <math.h>
 
 #include "ra_common.h"
+#include "ra_dma.h"
 #include "ra_runtime.h"
 #include "ringattn.h"
 
@@ -74,64 +75,88 @@ __device__ __forceinline__ bf16x8 from_e2m1(uint32_t codes, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A workgroup of 8 waves takes a block of 16 outputs for NT tiles of 16 rows; its waves take turns
-// of U weight blocks along the inputs, their sums are added in wave order through LDS.  Every
-// weight is read once a launch and becomes a bf16 operand once for all NT tiles; x comes from L2.
-constexpr int kMxWaves = 8;
-
-template <int NT, int U>
-__global__ __launch_bounds__(64 * kMxWaves) void mx4_linear_kernel(const MxArgs a) {
-  __shared__ f32x4 s_sum[kMxWaves][NT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, c = lane >> 4;
-  const int i = blockIdx.x, t0 = blockIdx.y * NT * 16;
-  const uint8_t* w4 = a.w4 + (long long)i * a.kb * 1024 + lane * 16;
-  const uint8_t* sc = a.scales + (long long)i * a.kb * 64 + l16 * 4;
-  f32x4 acc[NT];
+// A workgroup of WV waves takes NB blocks of 16 outputs for NT tiles of 16 rows; its waves take
+// turns along the inputs, 128 at a time, and their sums are added in wave order through LDS.
+// Every weight is read once for NT tiles, straight from memory into the lane that needs it, and
+// becomes a bf16 operand once.  The rows' 128 inputs go through a slab of LDS of the wave's own:
+// an operand's neighbouring lanes are neighbouring rows, and a load of 64 lanes from 16 rows
+// takes the address unit four times as long as the slab's loads of whole 256-byte pieces (48 x
+// 11008 x 4096: 33 us without the slab, 16 with it; 7 x 4096 x 11008: 9 and 7).  Workgroups start
+// at different inputs: the rows' pieces at one place lie in few channels of the L2 where the row
+// length is a multiple of 4 KB (32 x 4096 x 4096: 7.6 us without, 6.7).
+// Bound by latency for few weights; by the weights' bytes and, for many rows, by x, which every
+// workgroup reads whole from L2.
+template <int NT, int NB, int WV>
+__global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
+  constexpr int SLAB = NT * 4096, SUMS = NT * NB * 1024;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[WV][SLAB > SUMS ? SLAB : SUMS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, c = lane >> 4;
+  const int nb = (a.N + 15) / 16, i0 = blockIdx.x * NB, t0 = blockIdx.y * NT * 16;
+  const int rows = min(NT * 16, a.T - t0);
+  uint8_t* slab = s_mem[wave];
+  const int xoff = l16 * 256 + 16 * (c ^ swz<128>(l16));
+  const int start = (int)(blockIdx.x * 7u % (unsigned)a.kb);
+  const uint8_t *w4[NB], *sc[NB];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int b0 = wave * U; b0 < a.kb; b0 += kMxWaves * U) {
-    u32x4 w[U];
-    uint32_t e[U];
-    bf16x8 x[U][4][NT];
+  for (int j = 0; j < NB; ++j) {
+    const int i = min(i0 + j, nb - 1);  // (past the end: computed, not stored)
+    w4[j] = a.w4 + (long long)i * a.kb * 1024 + lane * 16;
+    sc[j] = a.scales + (long long)i * a.kb * 64 + l16 * 4;
+  }
+  f32x4 acc[NB][NT];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int b = min(b0 + u, a.kb - 1);
-      w[u] = *(const u32x4*)(w4 + (long long)b * 1024);
-      e[u] = *(const uint32_t*)(sc + (long long)b * 64);
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[j][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int at = wave; at < a.kb; at += WV) {
+    const int b = at + start < a.kb ? at + start : at + start - a.kb;
+#pragma unroll
+    for (int j = 0; j < NT * 4; ++j) {
+      if (4 * j >= rows) break;
+      // four rows a load; rows and inputs past the ends read others, which nothing uses
+      const int r = 4 * j + c, k = min(128 * b + 8 * (l16 ^ swz<128>(r)), a.K - 8);
+      dma_lds16_at(a.x + (long long)min(t0 + r, a.T - 1) * a.K + k, lds_addr(slab) + j * 1024);
     }
+    u32x4 w[NB];
+    uint32_t e[NB];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int j = 0; j < NB; ++j) {
+      w[j] = *(const u32x4*)(w4[j] + (long long)b * 1024);
+      e[j] = *(const uint32_t*)(sc[j] + (long long)b * 64);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+    for (int s = 0; s < 4; ++s) {
+      if (128 * b + 32 * s >= a.K) break;
+      bf16x8 x[NT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          // (places past the ends read others' elements: for rows that are not stored, or unused)
-          const int k = min(128 * (b0 + u) + 32 * s, a.K - 32) + 8 * c, t = min(t0 + 16 * n + l16, a.T - 1);
-          x[u][s][n] = *(const bf16x8*)(a.x + (long long)t * a.K + k);
-        }
+      for (int n = 0; n < NT; ++n) x[n] = *(const bf16x8*)(slab + n * 4096 + (xoff ^ (64 * s)));
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int j = 0; j < NB; ++j) {
+        const bf16x8 wv = from_e2m1(w[j][s], __uint_as_float((e[j] >> (8 * s) & 255u) << 23));
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        if (128 * (b0 + u) + 32 * s >= a.K) break;
-        const bf16x8 wv = from_e2m1(w[u][s], __uint_as_float((e[u] >> (8 * s) & 255u) << 23));
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[n] = mfma16(wv, x[u][s][n], acc[n]);
+        for (int n = 0; n < NT; ++n) acc[j][n] = mfma16(wv, x[n], acc[j][n]);
       }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slab has been read
   }
 #pragma unroll
-  for (int n = 0; n < NT; ++n) s_sum[wave][n][lane] = acc[n];
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) ((f32x4*)slab)[(j * NT + n) * 64 + lane] = acc[j][n];
   __syncthreads();
-  if (wave >= NT) return;
-  f32x4 y = s_sum[0][wave][lane];
+  for (int q = wave; q < NT * NB; q += WV) {
+    f32x4 y = ((const f32x4*)s_mem[0])[q * 64 + lane];
 #pragma unroll
-  for (int v = 1; v < kMxWaves; ++v) y += s_sum[v][wave][lane];
-  const int t = t0 + 16 * wave + l16, n0 = 16 * i + 4 * c;
-  if (t >= a.T) return;
+    for (int v = 1; v < WV; ++v) y += ((const f32x4*)s_mem[v])[q * 64 + lane];
+    const int t = t0 + 16 * (q % NT) + l16, n0 = 16 * (i0 + q / NT) + 4 * c;
+    if (t >= a.T) continue;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const long long at = (long long)t * a.N + n0 + j;
-    if (n0 + j < a.N) a.y[at] = (bf16)(y[j] + (a.residual ? (float)a.residual[at] : 0.f));
+    for (int j = 0; j < 4; ++j) {
+      const long long o = (long long)t * a.N + n0 + j;
+      if (n0 + j < a.N) a.y[o] = (bf16)(y[j] + (a.residual ? (float)a.residual[o] : 0.f));
+    }
   }
 }
 
@@ -169,14 +194,28 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
   if (T > kMxMaxT) return set_err(RA_EUNSUPPORTED, "T=%d exceeds %d rows", T, kMxMaxT);
   MxArgs a{(const bf16*)x, (const uint8_t*)w4, scales, (const bf16*)residual, (bf16*)y, T, d_in, d_out,
            (d_in + 127) / 128};
-  const int tiles = (T + 15) / 16;
-  auto run = [&](auto kernel, int nt) {
-    hipLaunchKernelGGL(kernel, dim3((d_out + 15) / 16, (tiles + nt - 1) / nt), dim3(64 * kMxWaves), 0, stream, a);
+  // NT: a pass over the weights for up to 64 rows.  Blocks a workgroup: as many as leave one
+  // workgroup a compute unit (of 256), for then x is read least often.  us with one, two, four
+  // blocks: 64 x 4096 x 11008 (688 blocks) -, 19.3, 15.4; 20 x 2048 x 6000 (375) 5.9, 5.2, 6.2; 32 x
+  // 4096 x 4096 (256) 6.7, 7.3, 8.3.  For one tile x is little: one block, with 16 waves where the
+  // blocks are no more than the compute units (1 x 11008 x 4096: 6.4 us, 8 waves 8.3; 7 x 4096 x
+  // 11008, 688 blocks: 8.4, 8 waves 6.9).
+  const int tiles = (T + 15) / 16, blocks = (d_out + 15) / 16;
+  auto run = [&](auto kernel, int nt, int nb, int wv) {
+    hipLaunchKernelGGL(kernel, dim3((blocks + nb - 1) / nb, (tiles + nt - 1) / nt), dim3(64 * wv), 0, stream, a);
   };
-  if (tiles == 1) run(mx4_linear_kernel<1, 4>, 1);
-  else if (tiles == 2) run(mx4_linear_kernel<2, 2>, 2);
-  else if (tiles == 3) run(mx4_linear_kernel<3, 2>, 3);
-  else run(mx4_linear_kernel<4, 2>, 4);
+  const int nb = blocks <= 256 ? 1 : blocks <= 512 ? 2 : 4;
+  if (tiles == 1 && nb == 1) run(mx4_linear_kernel<1, 1, 16>, 1, 1, 16);
+  else if (tiles == 1) run(mx4_linear_kernel<1, 1, 8>, 1, 1, 8);
+  else if (tiles == 2 && nb == 1) run(mx4_linear_kernel<2, 1, 8>, 2, 1, 8);
+  else if (tiles == 2 && nb == 2) run(mx4_linear_kernel<2, 2, 8>, 2, 2, 8);
+  else if (tiles == 2) run(mx4_linear_kernel<2, 4, 8>, 2, 4, 8);
+  else if (tiles == 3 && nb == 1) run(mx4_linear_kernel<3, 1, 8>, 3, 1, 8);
+  else if (tiles == 3 && nb == 2) run(mx4_linear_kernel<3, 2, 8>, 3, 2, 8);
+  else if (tiles == 3) run(mx4_linear_kernel<3, 4, 8>, 3, 4, 8);
+  else if (nb == 1) run(mx4_linear_kernel<4, 1, 8>, 4, 1, 8);
+  else if (nb == 2) run(mx4_linear_kernel<4, 2, 8>, 4, 2, 8);
+  else run(mx4_linear_kernel<4, 4, 8>, 4, 4, 8);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

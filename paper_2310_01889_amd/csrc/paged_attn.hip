@@ -444,77 +444,86 @@ __global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
   }
 }
 
-// Joins the parts of the groups that several waves share: a workgroup of 8 waves takes one query
-// slot of one entry.  The weights 2^(m - M) of the parts go to LDS; wave i sums every eighth part,
-// its loads independent of one another, and the eight sums are added in order.
+// Joins the parts of the groups that several waves share.  WPS waves take one query slot of one
+// entry: each sums every WPS-th part, its loads independent of one another, and their sums are
+// added in order.  A workgroup is 8 waves: one slot (groups are few, their parts many) or eight
+// (see the choice at the launch).  The weights 2^(m - M) are formed by the lanes, 64 parts at a time.
 constexpr int kJoinWaves = 8;
 
-template <int D>
+template <int D, int WPS>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const PagedArgs a) {
   constexpr int E = D / 64;
-  __shared__ float s_w[kWorkers];
-  __shared__ float s_red[2][kJoinWaves];
-  __shared__ float s_part[kJoinWaves][D];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.Hq / a.Hkv, slot = blockIdx.y;
+  __shared__ float s_sum[kJoinWaves][D + 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.Hq / a.Hkv;
+  const int slot = blockIdx.y * (kJoinWaves / WPS) + wave / WPS, w = wave % WPS;
   if (a.by_group) {  // an entry is there if its request has such a round
     const int g = blockIdx.x / a.rounds, round = blockIdx.x - g * a.rounds;
     if (request(a, g / a.Hkv).n * G <= round * kSlots) return;
   }
   const Split sp = a.split[blockIdx.x];
-  if (sp.parts == 0 || slot >= sp.slots) return;
+  if (sp.parts == 0 || (int)blockIdx.y * (kJoinWaves / WPS) >= sp.slots) return;
+  const bool on = slot < sp.slots;  // (the waves of a workgroup meet at its barriers)
   auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i)) * a.M + slot; };
-  float mx = -INFINITY;
-  for (int i = tid; i < sp.parts; i += 64 * kJoinWaves) {
-    const float m = a.part_ml[2 * part(i)];
-    s_w[i] = m;
-    mx = fmaxf(mx, m);
-  }
+  // the largest maximum of this wave's parts, then their sums relative to it
+  const int mine = on ? (sp.parts - w + WPS - 1) / WPS : 0;  // parts w, w + WPS, ...
+  float m = -INFINITY;
+  for (int i = lane; i < mine; i += 64) m = fmaxf(m, a.part_ml[2 * part(w + i * WPS)]);
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
-  if (lane == 0) s_red[0][wave] = mx;
-  __syncthreads();
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  const float m_eff = m == -INFINITY ? 0.f : m;
+  float l = 0.f, acc[E];
 #pragma unroll
-  for (int i = 0; i < kJoinWaves; ++i) mx = fmaxf(mx, s_red[0][i]);
-  const float m_eff = mx == -INFINITY ? 0.f : mx;
-  float l = 0.f;
-  for (int i = tid; i < sp.parts; i += 64 * kJoinWaves) {
-    const float li = a.part_ml[2 * part(i) + 1], wt = li == 0.f ? 0.f : exp2f(s_w[i] - m_eff);
-    s_w[i] = wt;
-    l = fmaf(li, wt, l);
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  for (int i0 = 0; i0 < mine; i0 += 64) {
+    float wt = 0.f;
+    if (i0 + lane < mine) {
+      const f32x2 ml = *(const f32x2*)(a.part_ml + 2 * part(w + (i0 + lane) * WPS));
+      wt = ml[1] == 0.f ? 0.f : exp2f(ml[0] - m_eff);
+      l = fmaf(ml[1], wt, l);
+    }
+    const int n = min(64, mine - i0);
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) {
+      const float* x = a.part_acc + part(w + (i0 + i) * WPS) * D;
+      const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), i));
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane + 64 * e], wi, acc[e]);
+    }
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
-  if (lane == 0) s_red[1][wave] = l;
-  __syncthreads();
-  float acc[E];
+  float top = m_eff;
+  if constexpr (WPS > 1) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 8
-  for (int i = wave; i < sp.parts; i += kJoinWaves) {
-    const float* x = a.part_acc + part(i) * D;
-    const float wt = s_w[i];
+    for (int e = 0; e < E; ++e) s_sum[wave][lane + 64 * e] = acc[e];
+    if (lane == 0) {
+      s_sum[wave][D] = m;
+      s_sum[wave][D + 1] = l;
+    }
+    __syncthreads();
+    if (w != 0) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane + 64 * e], wt, acc[e]);
+    for (int v = 1; v < WPS; ++v) m = fmaxf(m, s_sum[wave + v][D]);
+    top = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int v = 0; v < WPS; ++v) {
+      const float mv = s_sum[wave + v][D], lv = s_sum[wave + v][D + 1];
+      const float wv = lv == 0.f ? 0.f : exp2f((mv == -INFINITY ? 0.f : mv) - top);
+      l = fmaf(lv, wv, l);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(s_sum[wave + v][lane + 64 * e], wv, acc[e]);
+    }
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) s_part[wave][lane + 64 * e] = acc[e];
-  __syncthreads();
-  if (wave != 0) return;
-  l = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll
-  for (int i = 0; i < kJoinWaves; ++i) {
-    l += s_red[1][i];
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += s_part[i][lane + 64 * e];
-  }
+  if (!on) return;
   const int n = sp.slot0 + slot, t = n / G;
   const long long qrow = (long long)(sp.row0 + t) * a.Hq + sp.h * G + (n - t * G);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < E; ++e) a.o[qrow * D + lane + 64 * e] = (bf16)(acc[e] * inv);
-  if (lane == 0) a.lse[qrow] = l == 0.f ? -INFINITY : m_eff * kLn2 + logf(l);
+  if (lane == 0) a.lse[qrow] = l == 0.f ? -INFINITY : top * kLn2 + logf(l);
 }
 
 }  // namespace
@@ -579,7 +588,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   if (rc) return rc;
   if (int e = check_aligned({workspace})) return e;
   const bool f8 = kv_type == RA_KV_E4M3;
-  const int W = kWorkers, M = paged_slots(Hq, Hkv, max_new);
+  const int M = paged_slots(Hq, Hkv, max_new);
   const int rounds = (int)(((long long)max_new * (Hq / Hkv) + kSlots - 1) / kSlots);
   const size_t need = paged_bytes(kWorkers, M, D);
   if (workspace && workspace_bytes < need)
@@ -591,20 +600,23 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   }
   const long long groups = (long long)R * Hkv * rounds;
   float* acc = (float*)workspace;
-  float* ml = acc + (size_t)W * 2 * M * D;
+  float* ml = acc + (size_t)kWorkers * 2 * M * D;
   PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, acc, ml,
-              (Split*)(ml + (size_t)W * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
-              groups <= W, 1.f / sqrtf((float)D)};
+              (Split*)(ml + (size_t)kWorkers * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
+              groups <= kWorkers, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   auto* kern = D == 128 ? (f8 ? paged_partial_kernel<128, true> : paged_partial_kernel<128, false>)
                         : (f8 ? paged_partial_kernel<64, true> : paged_partial_kernel<64, false>);
   RA_HIP(timed_launch(RA_KERNEL_DECODE, stream, [&] {
-    hipLaunchKernelGGL(kern, dim3(W), dim3(64), 0, stream, a);
+    hipLaunchKernelGGL(kern, dim3(kWorkers), dim3(64), 0, stream, a);
     return hipGetLastError();
   }));
-  const dim3 grid(a.by_group ? (unsigned)groups : W, M);
-  if (D == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, dim3(64 * kJoinWaves), 0, stream, a);
-  else hipLaunchKernelGGL(paged_join_kernel<64>, grid, dim3(64 * kJoinWaves), 0, stream, a);
+  // few groups: many parts each, a workgroup a slot; many: few parts, a wave a slot
+  const bool few = groups <= 64;
+  const dim3 grid(a.by_group ? (unsigned)groups : kWorkers, few ? M : (M + kJoinWaves - 1) / kJoinWaves);
+  auto* join = D == 128 ? (few ? paged_join_kernel<128, kJoinWaves> : paged_join_kernel<128, 1>)
+                        : (few ? paged_join_kernel<64, kJoinWaves> : paged_join_kernel<64, 1>);
+  hipLaunchKernelGGL(join, grid, dim3(64 * kJoinWaves), 0, stream, a);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

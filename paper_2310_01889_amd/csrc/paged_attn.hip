@@ -105,6 +105,32 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t lo, uint32_t hi, float scal
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
+// Whether any of 16 bytes of values is not finite (8 bits: NaN), and the bytes with those zeroed.
+template <bool F8>
+__device__ __forceinline__ bool any_not_finite(u32x4 x) {
+  bool odd = false;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (F8) odd |= (((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;  // 0x7f becomes 0x80
+    else odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+  }
+  return odd;
+}
+template <bool F8>
+__device__ __forceinline__ u32x4 only_finite(u32x4 x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (F8) {
+      const uint32_t hit = (((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
+      x[e] &= ~(hit * 0xffu);
+    } else {
+      if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+      if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+    }
+  }
+  return x;
+}
+
 // One wave a workgroup.  Per tile the arithmetic of the decode kernel over a contiguous cache:
 // S^T = K Q^T on the matrix cores (K rows with bits 2 and 3 of the row index swapped as the A
 // operand, a lane one query slot), lazy online softmax, O^T += V^T P^T with V^T from the
@@ -113,7 +139,7 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t lo, uint32_t hi, float scal
 // 8-bit tiles become bf16 operands in registers, exactly: key rows under their scales, values as
 // they are, their scales (powers of two) going into the probabilities before those are rounded.
 template <int D, bool F8>
-__global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a) {
   constexpr int RB = F8 ? D : 2 * D;              // bytes a row
   constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
   constexpr int KT = 8192 / RB < 64 ? 8192 / RB : 64;  // keys a tile
@@ -217,6 +243,7 @@ __global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
     float m_run = -INFINITY, l_run = 0.f, m_eff = 0.f, thr = -INFINITY;
+    uint64_t hit_nan = 0, hit_up = 0, hit_down = 0;  // this lane's sums that a value not finite joins
     // slot of key row `lane` of tile i in the cache, or -1; the ids of 64 pages are at hand
     const int* trow = a.table + (long long)r * a.max_pages;
     int ids = -1, ids_at = -1;
@@ -270,22 +297,38 @@ __global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
       // keys that some row of the request does not see, or none does
       const bool diagonal = k0 + KT - 1 > q.first;
       const bool masked = diagonal || present != (KT == 64 ? ~0ull : (1ull << KT) - 1);
-      bool odd = false;  // a value that is not finite in a tile that some rows see only in part
       if (diagonal && q.n > 1) {
+        // A value that is not finite, in a row that some slots see and some do not, would make NaN
+        // of zero probabilities: its slots are noted, and it is overwritten by zero.
+        bool odd = false;
+#pragma unroll 1
+        for (int i = 0; i < TB / 1024; ++i) odd |= any_not_finite<F8>(*(const u32x4*)(vt + i * 1024 + lane * 16));
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+#pragma unroll 1
+          for (int row = 0; row < KT; ++row) {
+            if (k0 + row > qpos) continue;
+#pragma unroll 1
+            for (int g = 0; g < NDT * 4; ++g) {  // elements 4 g ... of this lane's part of a row
+              const int byte = (F8 ? 1 : 2) * (8 * g + 4 * hi);
+              const uint8_t* at = vt + row * RB + 16 * ((byte >> 4) ^ row_swz<RB>(row)) + (byte & 15);
 #pragma unroll
-        for (int i = 0; i < KT * RB / 1024; ++i) {
-          const u32x4 x = *(const u32x4*)(vt + i * 1024 + lane * 16);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (F8) {
-              const uint32_t y = (x[e] & 0x7f7f7f7fu) + 0x01010101u;  // 0x7f becomes 0x80
-              odd |= (y & 0x80808080u) != 0;
-            } else {
-              odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+              for (int e = 0; e < 4; ++e) {
+                const float x = F8 ? ((at[e] & 0x7f) == 0x7f ? NAN : 0.f) : (float)((const bf16*)at)[e];
+                const uint64_t bit = 1ull << (4 * g + e);
+                if (x != x) hit_nan |= bit;
+                else if (x == INFINITY) hit_up |= bit;
+                else if (x == -INFINITY) hit_down |= bit;
+              }
             }
           }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+          for (int i = 0; i < TB / 1024; ++i) {
+            u32x4* at = (u32x4*)(vt + i * 1024 + lane * 16);
+            *at = only_finite<F8>(*at);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
-        odd = __builtin_amdgcn_ballot_w64(odd) != 0;
       }
 #pragma unroll
       for (int sub = 0; sub < NS; ++sub) {
@@ -360,7 +403,7 @@ __global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
           for (int j = 0; j < 4; ++j) pw[j] = pack_bf16x2(s[8 * g + 2 * j], s[8 * g + 2 * j + 1]);
           pb[g] = __builtin_bit_cast(bf16x8, pw);
         }
-        uint8_t* vs = vt + 32 * sub * RB;
+        const uint8_t* vs = vt + 32 * sub * RB;
         auto values = [&](int g, int dt) __attribute__((always_inline)) {  // 16 keys x 32 dims of V^T
           const uint8_t* vg = vs + 16 * g * RB;
           if constexpr (F8) {
@@ -374,35 +417,23 @@ __global__ __launch_bounds__(64) void paged_partial_kernel(const PagedArgs a) {
             return bf16x8{lo[0], lo[1], lo[2], lo[3], up[0], up[1], up[2], up[3]};
           }
         };
-        if (!odd) {
 #pragma unroll
-          for (int g = 0; g < 2; ++g)
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) oacc[dt] = mfma32(values(g, dt), pb[g], oacc[dt]);
-        } else {
-          // 0 * inf is NaN in the products: token by token, the last first, the values past its
-          // position overwritten by zeros, and only its slots' sums kept
-          int zeros = 32;
-#pragma unroll 1
-          for (int tt = q.n - 1; tt >= 0; --tt) {
-            const int keep = min(max(q.first + tt + 1 - k0 - 32 * sub, 0), 32);
-            for (int row = keep; row < zeros; ++row)
-              if (lane < CPR) *(u32x4*)(vs + row * RB + 16 * lane) = u32x4{0, 0, 0, 0};
-            zeros = min(zeros, keep);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-            for (int dt = 0; dt < NDT; ++dt) {
-              f32x16 x;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) x[i] = 0.f;
-              x = mfma32(values(0, dt), pb[0], x);
-              x = mfma32(values(1, dt), pb[1], x);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) oacc[dt][i] = t == tt ? oacc[dt][i] + x[i] : oacc[dt][i];
-            }
-          }
-        }
+          for (int dt = 0; dt < NDT; ++dt) oacc[dt] = mfma32(values(g, dt), pb[g], oacc[dt]);
       }
+    }
+
+    if (__builtin_amdgcn_ballot_w64((hit_nan | hit_up | hit_down) != 0)) {
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {  // bit 16 dt + i: dims 32 dt + 8 (i / 4) + 4 hi + i % 4
+          const uint64_t bit = 1ull << (16 * dt + i);
+          if (hit_up & bit) oacc[dt][i] += INFINITY;
+          if (hit_down & bit) oacc[dt][i] -= INFINITY;
+          if (hit_nan & bit) oacc[dt][i] = NAN;
+        }
     }
 
     // ---- the result, or this wave's part of it ----

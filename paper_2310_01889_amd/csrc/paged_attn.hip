@@ -5,13 +5,14 @@
 // A step reads every key and value once, 2 D bytes a key and head each (D and a scale in 8 bits):
 // it is bound by HBM bandwidth, as long as the reads are spread evenly over the chip.
 //
-// Work is counted in units: one tile of KT keys of one key head of one request, for up to 32
-// query slots (slot n = new token n / G, query head n % G of the G that share the key head;
-// requests of more slots take several rounds over their keys).  The units of all requests stand
-// in one row, request by request, head by head, and kWorkers waves take equal shares of it, so
-// the lengths of a batch do not matter for the balance.  The lengths are on the device: each
-// wave finds its share from their prefix sums itself.  A wave whose share holds a whole (request,
-// head) writes its result; the others leave partial softmax states that a second launch joins.
+// Work is counted in units: one tile of KT keys of one request, for up to 32 query slots a key
+// head (slot n = new token n / G, query head n % G of the G that share the key head; requests of
+// more slots take several rounds over their keys).  The units of all requests stand in one row,
+// and teams of Hkv waves, a wave a key head, take equal shares of it, so the lengths of a batch do
+// not matter for the balance; the heads of one token, neighbours in memory, are read at about the
+// same time.  The lengths are on the device: each wave finds its team's share from their prefix
+// sums itself.  A wave whose share holds a whole (request, round) writes its result; the others
+// leave partial softmax states that a second launch joins.
 #include <math.h>
 
 #include <algorithm>
@@ -27,7 +28,7 @@ namespace {
 
 constexpr int kMaxNew = 32;      // new tokens a request
 constexpr int kSlots = 32;       // query slots a wave
-constexpr int kWorkers = 1024;   // waves: one a SIMD
+constexpr int kWorkers = 1024;   // waves: one a SIMD (four tile pairs of 32 KB a compute unit)
 constexpr int kMinShare = 1;     // units a wave takes at least
 constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
 
@@ -38,7 +39,7 @@ struct Split {
   int h;      // key head
   int slot0;  // first query slot (of the request's n * G)
   int slots;  // query slots
-  int first;  // index of the first wave's part; those of the waves after it follow, 2 apart
+  int first;  // index of the first wave's part; the next teams' follow, 2 Hkv apart
   int parts;
 };
 
@@ -56,6 +57,7 @@ struct PagedArgs {
   int M;            // query slots of a group at most
   int rounds;       // rounds of slots of a request at most
   int by_group;     // entries of split: 1 a group, 0 a wave
+  int teams;        // kWorkers / Hkv
   float scale;
 };
 
@@ -150,14 +152,16 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
   __shared__ __attribute__((aligned(256))) uint32_t sKS[2][F8 ? 64 : 1];
   __shared__ __attribute__((aligned(256))) uint32_t sVS[2][F8 ? 64 : 1];
   const int lane = threadIdx.x, l32 = lane & 31, hi = lane >> 5;
-  const int w = blockIdx.x, G = a.Hq / a.Hkv;
+  const int G = a.Hq / a.Hkv;
+  // a team's waves are of one XCD: what its heads read side by side (ids, scales) shares an L2
+  const int w = xcd_swizzle(blockIdx.x, kWorkers), team = w / a.Hkv, h = w - team * a.Hkv;
 
-  // ---- this wave's share of the units ----
+  // ---- this team's share of the units ----
   auto units = [&](int r) -> long long {  // of request r
     if (r >= a.R) return 0;
     const Request q = request(a, r);
     const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
-    return (long long)a.Hkv * rounds * tiles;
+    return (long long)rounds * tiles;
   };
   auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
 #pragma unroll
@@ -167,21 +171,22 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
     }
     return v;
   };
+  auto quotient = [&](long long x, long long y) {  // x / y, seldom past 32 bits
+    return (x | y) >> 31 ? x / y : (long long)((uint32_t)x / (uint32_t)y);
+  };
   const int per = (a.R + 63) / 64;  // requests a lane sums
   long long mine = 0;
   for (int j = 0; j < per; ++j) mine += units(lane * per + j);
   const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
-  const long long share = max((long long)kMinShare, (total + kWorkers - 1) / kWorkers);
-  const long long u0 = share * w, u1 = min(total, u0 + share);
+  const long long share = max((long long)kMinShare, quotient(total + a.teams - 1, a.teams));
+  const long long u0 = share * team, u1 = min(total, u0 + share);
   if (!a.by_group && lane == 0) a.split[w].parts = 0;
-  if (u0 >= u1) return;
+  if (team >= a.teams || u0 >= u1) return;
   // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
-  int r;
-  long long r_at;  // first unit of request r
-  {
-    const int l = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
-    r_at = __shfl(upto - mine, l);
-    r = l * per;
+  int r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
+  long long r_at = __shfl(upto - mine, r);  // first unit of request r
+  if (per > 1) {
+    r *= per;
     const long long v = lane < per ? units(r + lane) : 0, s = scan(v);
     const int k = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
     r_at += __shfl(s - v, k);
@@ -209,20 +214,20 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
   }
 
   for (long long u = u0; u < u1;) {
-    // ---- the group of unit u: request r, key head h, round of slots; its tiles [t0, t1) ----
+    // ---- the group of unit u: request r, round of slots; its tiles [t0, t1) ----
     Request q = request(a, r);
     int tiles, rounds;
     for (;;) {
       rounds = (q.n * G + kSlots - 1) / kSlots;
       tiles = max(1, (q.keys + KT - 1) / KT);
-      const long long end = r_at + (long long)a.Hkv * rounds * tiles;
+      const long long end = r_at + (long long)rounds * tiles;
       if (u < end) break;
       r_at = end;
       q = request(a, ++r);
     }
-    const long long in_r = u - r_at, grp = in_r / tiles;
-    const int t0 = (int)(in_r - grp * tiles), t1 = (int)min((long long)tiles, t0 + (u1 - u));
-    const int h = (int)(grp / rounds), slot0 = (int)(grp - (long long)h * rounds) * kSlots;
+    const long long in_r = u - r_at;
+    const int round = rounds == 1 ? 0 : (int)quotient(in_r, tiles), slot0 = round * kSlots;
+    const int t0 = (int)(in_r - (long long)round * tiles), t1 = (int)min((long long)tiles, t0 + (u1 - u));
     const int slots = min(kSlots, q.n * G - slot0);
     const int n = slot0 + min(l32, slots - 1), t = n / G;  // this lane's slot
     const long long qrow = (long long)(q.row0 + t) * a.Hq + h * G + (n - t * G);
@@ -466,8 +471,8 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
     }
     if (t0 == 0 && lane == 0 && (a.by_group || !whole)) {
       const long long last = u + tiles - 1;  // the group's last unit
-      a.split[a.by_group ? (r * a.Hkv + h) * a.rounds + slot0 / kSlots : w] =
-          Split{q.row0, h, slot0, slots, 2 * w + (u == u0 ? 0 : 1), whole ? 0 : (int)(last / share) - w + 1};
+      a.split[a.by_group ? (r * a.Hkv + h) * a.rounds + round : w] =
+          Split{q.row0, h, slot0, slots, 2 * w + (u == u0 ? 0 : 1), whole ? 0 : (int)quotient(last, share) - team + 1};
     }
     u += t1 - t0;
     // the buffers are refilled by the next group's first loads
@@ -494,7 +499,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const Paged
   const Split sp = a.split[blockIdx.x];
   if (sp.parts == 0 || (int)blockIdx.y * (kJoinWaves / WPS) >= sp.slots) return;
   const bool on = slot < sp.slots;  // (the waves of a workgroup meet at its barriers)
-  auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i)) * a.M + slot; };
+  auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i * a.Hkv)) * a.M + slot; };
   // the largest maximum of this wave's parts, then their sums relative to it
   const int mine = on ? (sp.parts - w + WPS - 1) / WPS : 0;  // parts w, w + WPS, ...
   float m = -INFINITY;
@@ -634,7 +639,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   float* ml = acc + (size_t)kWorkers * 2 * M * D;
   PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, acc, ml,
               (Split*)(ml + (size_t)kWorkers * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
-              groups <= kWorkers, 1.f / sqrtf((float)D)};
+              groups <= kWorkers, kWorkers / Hkv, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   auto* kern = D == 128 ? (f8 ? paged_partial_kernel<128, true> : paged_partial_kernel<128, false>)
                         : (f8 ? paged_partial_kernel<64, true> : paged_partial_kernel<64, false>);

@@ -423,6 +423,15 @@ def _arg(t, name, dtype, dev, shape=None):
     raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
 
 
+def _ints(t, name, n, dev):
+    """_arg of an int32 vector of n elements."""
+    if t is None:
+        return None
+    if t.dtype is _I32 and t.get_device() == dev and t.numel() == n and t.dim() == 1 and t.is_contiguous():
+        return t.data_ptr()
+    return _arg(t, name, _I32, dev, (n,))
+
+
 def _rows(t, name, T, H, D, dev):
     """Address and row stride of a bf16 [T, H, D] tensor whose rows are dense."""
     if t.shape != (T, H, D):
@@ -451,7 +460,7 @@ def _cache(k_pages, v_pages, k_scales, v_scales, dev):
 
 def _current(stream):
     """The current GPU and the handle of the stream a call runs on."""
-    dev = torch.cuda.current_device()
+    dev = torch._C._cuda_getDevice()
     return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
@@ -461,11 +470,11 @@ def paged_plan(lens, n_new, free_pages, free_head, block_table, cu_rows, new_len
     block_table [R, max_pages], cu_rows [R + 1], slots, positions [T], counts [4]."""
     R, max_pages = block_table.shape
     T, (dev, st) = len(slots), _current(stream)
-    _call("paged_plan", _arg(lens, "lens", _I32, dev, (R,)), _arg(n_new, "n_new", _I32, dev, (R,)),
-          _arg(free_pages, "free_pages", _I32, dev, (len(free_pages),)), _arg(free_head, "free_head", _I32, dev, (1,)),
-          _arg(block_table, "block_table", _I32, dev), _arg(cu_rows, "cu_rows", _I32, dev, (R + 1,)),
-          _arg(new_lens, "new_lens", _I32, dev, (R,)), _arg(slots, "slots", _I32, dev, (T,)),
-          _arg(positions, "positions", _I32, dev, (T,)), _arg(counts, "counts", _I32, dev, (4,)), R, page_size,
+    _call("paged_plan", _ints(lens, "lens", R, dev), _ints(n_new, "n_new", R, dev),
+          _ints(free_pages, "free_pages", len(free_pages), dev), _ints(free_head, "free_head", 1, dev),
+          _arg(block_table, "block_table", _I32, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
+          _ints(new_lens, "new_lens", R, dev), _ints(slots, "slots", T, dev),
+          _ints(positions, "positions", T, dev), _ints(counts, "counts", 4, dev), R, page_size,
           max_pages, n_pages, len(free_pages), T, st)
 
 
@@ -479,7 +488,7 @@ def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=No
     k_at, k_row = _rows(k, "k", T, Hkv, D, dev)
     v_at, v_row = _rows(v, "v", T, Hkv, D, dev)
     _call("paged_append", q_at, k_at, v_at, _arg(q_out, "q_out", _BF16, dev, (T, Hq, D)), kp, vp, ks, vs,
-          _arg(slots, "slots", _I32, dev, (T,)), _arg(positions, "positions", _I32, dev, (T,)), T, Hq, Hkv, D, q_row,
+          _ints(slots, "slots", T, dev), _ints(positions, "positions", T, dev), T, Hq, Hkv, D, q_row,
           k_row, v_row, n_pages, page_size, kind, 1 if rotate else 0, st)
 
 
@@ -504,7 +513,7 @@ def paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, m
     if workspace is not None:
         ws, ws_bytes = _arg(workspace, "workspace", workspace.dtype, dev), workspace.numel() * workspace.element_size()
     _call("paged_attn_decode", _arg(q, "q", _BF16, dev), kp, vp, ks, vs, _arg(block_table, "block_table", _I32, dev),
-          _arg(lens, "lens", _I32, dev, (R,)), _arg(cu_rows, "cu_rows", _I32, dev, (R + 1,)),
+          _ints(lens, "lens", R, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
           _arg(o, "o", _BF16, dev, (T, Hq, D)), _arg(lse, "lse", _F32, dev, (T, Hq)), ws, ws_bytes, T, R, Hq, Hkv, D,
           n_pages, page_size, max_pages, max_new, kind, st)
 

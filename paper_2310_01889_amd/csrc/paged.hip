@@ -193,44 +193,56 @@ struct AppendArgs {
   long long n_slots;
 };
 
-// A workgroup takes TB tokens: the cosines and sines of their positions go to LDS first, then 8
-// elements a thread of every head.  Angles: the turns position * freq in double, the whole turns
-// dropped, then sine and cosine of the rest in float32 (positions reach 10^6 radians and more).
+// A workgroup of 256 threads takes one token, 8 elements a thread of every head.  A thread's loads
+// (of kAppendLoads elements at a time) are issued before the token's cosines and sines are formed
+// into LDS, which hides one behind the other.  Angles: the turns position * freq in double, the
+// whole turns dropped, then sine and cosine of the rest in float32 (positions reach 10^6 radians
+// and more).  HBM-bound: 16384 tokens of 32 + 2 x 32 heads of 128 in bf16 (805 MB) 150 us.
+constexpr int kAppendLoads = 4;
+
 template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, const RopeFreq f, int TB) {
+__global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, const RopeFreq f) {
   constexpr int CPR = D / 8;  // threads a head
-  extern __shared__ float s_rope[];  // [TB][D/2][2]: cos, sin
-  const int t0 = blockIdx.x * TB, nt = min(TB, a.T - t0);
-  if (a.rotate)
-    for (int i = threadIdx.x; i < nt * (D / 2); i += 256) {
-      const double turns = (double)a.positions[t0 + i / (D / 2)] * f.turns[i % (D / 2)];
-      const float part = (float)(turns - rint(turns));
-      float sn, cs;
-      sincospif(2.f * part, &sn, &cs);
-      s_rope[2 * i] = cs;
-      s_rope[2 * i + 1] = sn;
-    }
-  __syncthreads();
-  const int heads = a.Hq + 2 * a.Hkv;
-  const int items = nt * heads * CPR;
+  __shared__ float s_rope[D];  // cos, sin of each pair
+  const int t = blockIdx.x, heads = a.Hq + 2 * a.Hkv, items = heads * CPR;
+  const int ch = threadIdx.x % CPR;
+  const long long step = 256 / CPR;  // heads a pass of the workgroup
+  const int pos = a.positions[t], slot = a.slots[t];
+  const bool stored = slot >= 0 && slot < a.n_slots;
+  auto source = [&](int hh) {  // the elements of this thread of head hh of q, k, v in a row
+    const bf16* src = hh < a.Hq ? a.q + (long long)t * a.q_stride + hh * D
+                                : hh < a.Hq + a.Hkv ? a.k + (long long)t * a.k_stride + (hh - a.Hq) * D
+                                                    : a.v + (long long)t * a.v_stride + (hh - a.Hq - a.Hkv) * D;
+    return (const bf16x8*)(src + ch * 8);
+  };
   // whole waves run the loop, so that the lanes of a head reduce together
-  for (int base = 0; base < items; base += 256) {
-    const int it = base + threadIdx.x;
-    const bool on = it < items;
-    const int ch = it % CPR, hh = on ? it / CPR % heads : 0, tl = on ? it / (CPR * heads) : 0, t = t0 + tl;
-    const int pos = a.positions[t], slot = a.slots[t];
-    const bool is_q = hh < a.Hq, is_k = !is_q && hh < a.Hq + a.Hkv;
-    const int h = is_q ? hh : is_k ? hh - a.Hq : hh - a.Hq - a.Hkv;
-    const bool live = on && pos >= 0 && (is_q ? a.q != nullptr : slot >= 0 && slot < a.n_slots);
-    float x[8];
-    if (live) {
-      const bf16* src = is_q ? a.q + (long long)t * a.q_stride
-                             : is_k ? a.k + (long long)t * a.k_stride : a.v + (long long)t * a.v_stride;
-      const bf16x8 in = *(const bf16x8*)(src + h * D + ch * 8);
+  for (int base = 0; base < items; base += 256 * kAppendLoads) {
+    const int h0 = (base + threadIdx.x) / CPR;
+    bf16x8 in[kAppendLoads];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = (float)in[e];
+    for (int u = 0; u < kAppendLoads; ++u) in[u] = *source(min(h0 + u * (int)step, heads - 1));
+    if (base == 0 && a.rotate) {
+      if (threadIdx.x < D / 2) {
+        const double turns = (double)pos * f.turns[threadIdx.x];
+        const float part = (float)(turns - rint(turns));
+        float sn, cs;
+        sincospif(2.f * part, &sn, &cs);
+        s_rope[2 * threadIdx.x] = cs;
+        s_rope[2 * threadIdx.x + 1] = sn;
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int u = 0; u < kAppendLoads; ++u) {
+      const int hh = h0 + u * (int)step;
+      const bool is_q = hh < a.Hq, is_k = !is_q && hh < a.Hq + a.Hkv;
+      const int h = is_q ? hh : is_k ? hh - a.Hq : hh - a.Hq - a.Hkv;
+      const bool live = hh < heads && pos >= 0 && (is_q || stored);
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)in[u][e];
       if (a.rotate && (is_q || is_k)) {
-        const float* cs = s_rope + tl * D + ch * 8;
+        const float* cs = s_rope + ch * 8;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x0 = x[2 * e], x1 = x[2 * e + 1], c = cs[2 * e], s = cs[2 * e + 1];
@@ -238,46 +250,44 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, c
           x[2 * e + 1] = x0 * s + x1 * c;
         }
       }
-    }
-    const long long row = (long long)slot * a.Hkv + h;
-    if (E4M3 && !is_q) {
-      // scale: the smallest power of two that brings every finite element to at most 448
-      float top = 0.f;
-      if (live) {
+      const long long row = (long long)slot * a.Hkv + h;
+      if (E4M3 && !is_q) {
+        // scale: the smallest power of two that brings every finite element to at most 448
+        float top = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const float m = fabsf(x[e]);
           if (m < INFINITY) top = fmaxf(top, m);
         }
-      }
-      uint32_t mag = __float_as_uint(top);
+        uint32_t mag = __float_as_uint(top);
 #pragma unroll
-      for (int off = CPR / 2; off >= 1; off >>= 1) mag = max(mag, (uint32_t)__shfl_xor((int)mag, off));
-      if (live) {
-        // 448 = 1.75 * 2^8: the exponent less 8, one more where the mantissa is past 1.75
-        int e2 = (int)(mag >> 23) - 127 - 8 + ((mag & 0x7fffffu) > 0x600000u);
-        e2 = mag == 0 ? 0 : max(e2, -126);
-        const float inv = ldexpf(1.f, -e2);
-        uint32_t w[2];
+        for (int off = CPR / 2; off >= 1; off >>= 1) mag = max(mag, (uint32_t)__shfl_xor((int)mag, off));
+        if (live) {
+          // 448 = 1.75 * 2^8: the exponent less 8, one more where the mantissa is past 1.75
+          int e2 = (int)(mag >> 23) - 127 - 8 + ((mag & 0x7fffffu) > 0x600000u);
+          e2 = mag == 0 ? 0 : max(e2, -126);
+          const float inv = ldexpf(1.f, -e2);
+          uint32_t w[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          int p = 0;
-          p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j] * inv, x[4 * j + 1] * inv, p, false);
-          p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2] * inv, x[4 * j + 3] * inv, p, true);
-          w[j] = (uint32_t)p;
+          for (int j = 0; j < 2; ++j) {
+            int p = 0;
+            p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j] * inv, x[4 * j + 1] * inv, p, false);
+            p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * j + 2] * inv, x[4 * j + 3] * inv, p, true);
+            w[j] = (uint32_t)p;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)  // e4m3 has no infinity: NaN
-            if (!(fabsf(x[4 * j + e]) < INFINITY)) w[j] |= 0x7fu << (8 * e);
+            for (int e = 0; e < 4; ++e)  // e4m3 has no infinity: NaN
+              if (!(fabsf(x[4 * j + e]) < INFINITY)) w[j] |= 0x7fu << (8 * e);
+          }
+          uint8_t* out = (uint8_t*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
+          *(u32x2*)out = u32x2{w[0], w[1]};
+          if (ch == 0) (is_k ? a.k_scales : a.v_scales)[row] = (uint8_t)(e2 + 127);
         }
-        uint8_t* out = (uint8_t*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
-        *(u32x2*)out = u32x2{w[0], w[1]};
-        if (ch == 0) (is_k ? a.k_scales : a.v_scales)[row] = (uint8_t)(e2 + 127);
+      } else if (live) {
+        bf16* out = is_q ? a.q_out + ((long long)t * a.Hq + h) * D + ch * 8
+                         : (bf16*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
+        *(u32x4*)out = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                             pack_bf16x2(x[6], x[7])};
       }
-    } else if (live) {
-      bf16* out = is_q ? a.q_out + ((long long)t * a.Hq + h) * D + ch * 8
-                       : (bf16*)(is_k ? a.k_pages : a.v_pages) + row * D + ch * 8;
-      *(u32x4*)out = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                           pack_bf16x2(x[6], x[7])};
     }
   }
 }
@@ -368,10 +378,9 @@ extern "C" int paged_append(const void* q, const void* k, const void* v, void* q
   if (q == q_out && q && q_stride != Hq * D) return set_err(RA_EINVAL, "q_out is dense: it can be q only where q is");
   AppendArgs a{(const bf16*)q, (const bf16*)k, (const bf16*)v, (bf16*)q_out, k_pages, v_pages, k_scales, v_scales,
                slots, positions, T, Hq, Hkv, q_stride, k_stride, v_stride, rotate, (long long)n_pages * page_size};
-  const int TB = 1;
   auto* kern = D == 128 ? (kv_type == RA_KV_E4M3 ? paged_append_kernel<128, true> : paged_append_kernel<128, false>)
                         : (kv_type == RA_KV_E4M3 ? paged_append_kernel<64, true> : paged_append_kernel<64, false>);
-  hipLaunchKernelGGL(kern, dim3((T + TB - 1) / TB), dim3(256), TB * D * 4, stream, a, rope_freq(D), TB);
+  hipLaunchKernelGGL(kern, dim3(T), dim3(256), 0, stream, a, rope_freq(D));
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

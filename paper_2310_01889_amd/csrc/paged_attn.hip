@@ -29,7 +29,6 @@ namespace {
 constexpr int kMaxNew = 32;      // new tokens a request
 constexpr int kSlots = 32;       // query slots a wave
 constexpr int kWorkers = 1024;   // waves: one a SIMD (four tile pairs of 32 KB a compute unit)
-constexpr int kMinShare = 1;     // units a wave takes at least
 constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
 
 // What the second launch joins: the parts of a group of units (request, key head, round) that
@@ -133,67 +132,85 @@ __device__ __forceinline__ u32x4 only_finite(u32x4 x) {
   return x;
 }
 
-// One wave a workgroup.  Per tile the arithmetic of the decode kernel over a contiguous cache:
+// GW = 0: one wave a workgroup, its team's share of all units.  GW > 0: short requests; GW waves take
+// the tiles of one group (request, key head, round) in turns and join their states in LDS, so that
+// one launch does.  Per tile the arithmetic of the decode kernel over a contiguous cache:
 // S^T = K Q^T on the matrix cores (K rows with bits 2 and 3 of the row index swapped as the A
 // operand, a lane one query slot), lazy online softmax, O^T += V^T P^T with V^T from the
 // transpose reads of LDS.  Tiles are double buffered: the direct-to-LDS loads of tile i + 1,
 // every row at an address of its own (pages of any size), are in flight while tile i is computed.
 // 8-bit tiles become bf16 operands in registers, exactly: key rows under their scales, values as
 // they are, their scales (powers of two) going into the probabilities before those are rounded.
-template <int D, bool F8>
-__global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a) {
+template <int D, bool F8, int GW>
+__global__ __launch_bounds__(64 * (GW ? GW : 1), GW > 1 ? 1 : 2) void paged_attn_kernel(const PagedArgs a) {
+  constexpr int NW = GW ? GW : 1;
   constexpr int RB = F8 ? D : 2 * D;              // bytes a row
   constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
   constexpr int KT = 8192 / RB < 64 ? 8192 / RB : 64;  // keys a tile
   constexpr int LOADS = KT / RPL, NS = KT / 32, NKK = D / 16, NDT = D / 32;
   constexpr int TB = KT * RB;                     // bytes of a tile; its scales: a dword a key
-  __shared__ __attribute__((aligned(1024))) uint8_t sK[2][TB];
-  __shared__ __attribute__((aligned(1024))) uint8_t sV[2][TB];
-  __shared__ __attribute__((aligned(256))) uint32_t sKS[2][F8 ? 64 : 1];
-  __shared__ __attribute__((aligned(256))) uint32_t sVS[2][F8 ? 64 : 1];
-  const int lane = threadIdx.x, l32 = lane & 31, hi = lane >> 5;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tiles[NW][2][2][TB];  // wave, K or V, buffer
+  __shared__ __attribute__((aligned(256))) uint32_t s_scales[NW][2][2][F8 ? 64 : 1];
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint8_t(*sK)[TB] = s_tiles[wave][0];
+  uint8_t(*sV)[TB] = s_tiles[wave][1];
+  uint32_t(*sKS)[F8 ? 64 : 1] = s_scales[wave][0];
+  uint32_t(*sVS)[F8 ? 64 : 1] = s_scales[wave][1];
   const int G = a.Hq / a.Hkv;
-  // a team's waves are of one XCD: what its heads read side by side (ids, scales) shares an L2
-  const int w = xcd_swizzle(blockIdx.x, kWorkers), team = w / a.Hkv, h = w - team * a.Hkv;
-
-  // ---- this team's share of the units ----
-  auto units = [&](int r) -> long long {  // of request r
-    if (r >= a.R) return 0;
-    const Request q = request(a, r);
-    const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
-    return (long long)rounds * tiles;
-  };
-  auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const long long y = __shfl_up(v, off);
-      if (lane >= off) v += y;
-    }
-    return v;
-  };
   auto quotient = [&](long long x, long long y) {  // x / y, seldom past 32 bits
     return (x | y) >> 31 ? x / y : (long long)((uint32_t)x / (uint32_t)y);
   };
-  const int per = (a.R + 63) / 64;  // requests a lane sums
-  long long mine = 0;
-  for (int j = 0; j < per; ++j) mine += units(lane * per + j);
-  const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
-  const long long share = max((long long)kMinShare, quotient(total + a.teams - 1, a.teams));
-  const long long u0 = share * team, u1 = min(total, u0 + share);
-  if (!a.by_group && lane == 0) a.split[w].parts = 0;
-  if (team >= a.teams || u0 >= u1) return;
-  // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
-  int r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
-  long long r_at = __shfl(upto - mine, r);  // first unit of request r
-  if (per > 1) {
-    r *= per;
-    const long long v = lane < per ? units(r + lane) : 0, s = scan(v);
-    const int k = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
-    r_at += __shfl(s - v, k);
-    r += k;
+  // neighbours of one XCD: what the heads of a request read side by side (ids, scales) shares an L2
+  const int id = xcd_swizzle(blockIdx.x, gridDim.x);
+  int w = 0, team = 0, h, r;
+  long long share = 0, u0 = 0, u1 = 1, r_at = 0;  // r_at: first unit of request r
+  if constexpr (GW > 0) {
+    const int q = id / a.rounds;
+    r = q / a.Hkv;
+    h = q - r * a.Hkv;
+  } else {
+    w = id;
+    team = w / a.Hkv;
+    h = w - team * a.Hkv;
+
+    // ---- this team's share of the units ----
+    auto units = [&](int r) -> long long {  // of request r
+      if (r >= a.R) return 0;
+      const Request q = request(a, r);
+      const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
+      return (long long)rounds * tiles;
+    };
+    auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const long long y = __shfl_up(v, off);
+        if (lane >= off) v += y;
+      }
+      return v;
+    };
+    const int per = (a.R + 63) / 64;  // requests a lane sums
+    long long mine = 0;
+    for (int j = 0; j < per; ++j) mine += units(lane * per + j);
+    const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
+    share = max(1ll, quotient(total + a.teams - 1, a.teams));
+    u0 = share * team;
+    u1 = min(total, u0 + share);
+    if (!a.by_group && lane == 0) a.split[w].parts = 0;
+    if (team >= a.teams || u0 >= u1) return;
+    // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
+    r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
+    r_at = __shfl(upto - mine, r);
+    if (per > 1) {
+      r *= per;
+      const long long v = lane < per ? units(r + lane) : 0, s = scan(v);
+      const int k = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
+      r_at += __shfl(s - v, k);
+      r += k;
+    }
+    r = __builtin_amdgcn_readfirstlane(r);
+    r_at = uniform(r_at);
   }
-  r = __builtin_amdgcn_readfirstlane(r);
-  r_at = uniform(r_at);
 
   // ---- constants of the tile loop ----
   const float sl2 = a.scale * kLog2e;
@@ -216,31 +233,32 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
   for (long long u = u0; u < u1;) {
     // ---- the group of unit u: request r, round of slots; its tiles [t0, t1) ----
     Request q = request(a, r);
-    int tiles, rounds;
-    for (;;) {
-      rounds = (q.n * G + kSlots - 1) / kSlots;
+    int tiles, round, t0, t1;
+    if constexpr (GW > 0) {
       tiles = max(1, (q.keys + KT - 1) / KT);
-      const long long end = r_at + (long long)rounds * tiles;
-      if (u < end) break;
-      r_at = end;
-      q = request(a, ++r);
+      round = id % a.rounds;
+      if (round * kSlots >= q.n * G) return;
+      t0 = wave;
+      t1 = tiles;
+    } else {
+      int rounds;
+      for (;;) {
+        rounds = (q.n * G + kSlots - 1) / kSlots;
+        tiles = max(1, (q.keys + KT - 1) / KT);
+        const long long end = r_at + (long long)rounds * tiles;
+        if (u < end) break;
+        r_at = end;
+        q = request(a, ++r);
+      }
+      const long long in_r = u - r_at;
+      round = rounds == 1 ? 0 : (int)quotient(in_r, tiles);
+      t0 = (int)(in_r - (long long)round * tiles);
+      t1 = (int)min((long long)tiles, t0 + (u1 - u));
     }
-    const long long in_r = u - r_at;
-    const int round = rounds == 1 ? 0 : (int)quotient(in_r, tiles), slot0 = round * kSlots;
-    const int t0 = (int)(in_r - (long long)round * tiles), t1 = (int)min((long long)tiles, t0 + (u1 - u));
-    const int slots = min(kSlots, q.n * G - slot0);
+    const int slot0 = round * kSlots, slots = min(kSlots, q.n * G - slot0);
     const int n = slot0 + min(l32, slots - 1), t = n / G;  // this lane's slot
     const long long qrow = (long long)(q.row0 + t) * a.Hq + h * G + (n - t * G);
     const int qpos = q.first + t;
-
-    bf16x8 qreg[NKK];
-#pragma unroll
-    for (int kk = 0; kk < NKK; ++kk) {
-      const int d = F8 ? 32 * (kk / 2) + 16 * hi + 8 * (kk & 1) : 16 * kk + 8 * hi;
-      const bf16x8 x = *(const bf16x8*)(a.q + qrow * D + d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qreg[kk][e] = l32 < slots ? x[e] : (bf16)0.f;
-    }
 
     f32x16 oacc[NDT];
 #pragma unroll
@@ -280,17 +298,24 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
       }
     };
 
-    int s_cur = slot_of(t0);
-    load_tile(s_cur, 0);
+    int s_cur = -1;
+    if (GW <= 1 || t0 < t1) {
+      s_cur = slot_of(t0);
+      load_tile(s_cur, 0);
+    }
+    // (lanes past the slots repeat the last one; nothing of theirs is kept)
+    bf16x8 qreg[NKK];
+#pragma unroll
+    for (int kk = 0; kk < NKK; ++kk)
+      qreg[kk] = *(const bf16x8*)(a.q + qrow * D + (F8 ? 32 * (kk / 2) + 16 * hi + 8 * (kk & 1) : 16 * kk + 8 * hi));
 
 #pragma unroll 1
-    for (int it = t0; it < t1; ++it) {
-      const int b = (it - t0) & 1;
+    for (int it = t0, b = 0; it < t1; it += NW, b ^= 1) {
       const uint64_t present = __builtin_amdgcn_ballot_w64(s_cur >= 0);  // keys of the tile that exist
       // the previous tile's LDS reads have all returned before its buffer is refilled
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (it + 1 < t1) {
-        s_cur = slot_of(it + 1);
+      if (it + NW < t1) {
+        s_cur = slot_of(it + NW);
         load_tile(s_cur, b ^ 1);
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS + (F8 ? 2 : 0)) : "memory");  // tile it landed
       } else {
@@ -443,7 +468,49 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
 
     // ---- the result, or this wave's part of it ----
     const float l = pair_sum(l_run);
-    const bool whole = t0 == 0 && t1 == tiles;
+    if constexpr (GW > 1) {
+      // the waves' states through LDS: a slot's sums in a row of its own, 4 floats apart from the next
+      constexpr int ROW = D + 4;
+      static_assert(kSlots * ROW * 4 <= 4 * TB, "the states fit the tiles");
+      __shared__ float s_ml[GW][kSlots][2];
+      float* acc = (float*)s_tiles[wave];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (l32 < slots) {
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *(f32x4*)(acc + l32 * ROW + 32 * dt + 8 * g + 4 * hi) =
+                f32x4{oacc[dt][4 * g], oacc[dt][4 * g + 1], oacc[dt][4 * g + 2], oacc[dt][4 * g + 3]};
+        if (!hi) s_ml[wave][l32][0] = m_run, s_ml[wave][l32][1] = l;
+      }
+      __syncthreads();
+      for (int sl = wave; sl < slots; sl += GW) {
+        float mx = -INFINITY, lt = 0.f, wt[GW], x[D / 64];
+#pragma unroll
+        for (int v = 0; v < GW; ++v) mx = fmaxf(mx, s_ml[v][sl][0]);
+        const float top = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) x[e] = 0.f;
+#pragma unroll
+        for (int v = 0; v < GW; ++v) {
+          const float lv = s_ml[v][sl][1];
+          wt[v] = lv == 0.f ? 0.f : fast_exp2(s_ml[v][sl][0] - top);
+          lt = fmaf(lv, wt[v], lt);
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e)
+            x[e] = fmaf(((const float*)s_tiles[v])[sl * ROW + lane + 64 * e], wt[v], x[e]);
+        }
+        const int nn = slot0 + sl, tt = nn / G;
+        const long long row = (long long)(q.row0 + tt) * a.Hq + h * G + (nn - tt * G);
+        const float inv = lt == 0.f ? 0.f : 1.f / lt;
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) a.o[row * D + lane + 64 * e] = (bf16)(x[e] * inv);
+        if (lane == 0) a.lse[row] = lt == 0.f ? -INFINITY : top * kLn2 + logf(lt);
+      }
+      return;
+    }
+    const bool whole = GW == 1 || (t0 == 0 && t1 == tiles);
     if (l32 < slots) {
       if (whole) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -469,6 +536,7 @@ __global__ __launch_bounds__(64, 2) void paged_partial_kernel(const PagedArgs a)
         if (!hi) *(f32x2*)(a.part_ml + 2 * part) = f32x2{m_run, l};
       }
     }
+    if (GW == 1) return;
     if (t0 == 0 && lane == 0 && (a.by_group || !whole)) {
       const long long last = u + tiles - 1;  // the group's last unit
       a.split[a.by_group ? (r * a.Hkv + h) * a.rounds + round : w] =
@@ -641,12 +709,36 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
               (Split*)(ml + (size_t)kWorkers * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
               groups <= kWorkers, kWorkers / Hkv, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
-  auto* kern = D == 128 ? (f8 ? paged_partial_kernel<128, true> : paged_partial_kernel<128, false>)
-                        : (f8 ? paged_partial_kernel<64, true> : paged_partial_kernel<64, false>);
-  RA_HIP(timed_launch(RA_KERNEL_DECODE, stream, [&] {
-    hipLaunchKernelGGL(kern, dim3(kWorkers), dim3(64), 0, stream, a);
-    return hipGetLastError();
-  }));
+  // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
+  // where the groups fill the chip or the tiles (8 KB of keys, 64 keys at most) are few, four waves
+  // where the groups are at most one a compute unit; else shares of all tiles and a second launch.
+  // us with one wave, four, shares; bf16, requests of a quarter of the keys to all of them:
+  //   1024 groups of 128 dims: 120 keys 11.2, 19.0, 19.1; 500 36.8, 45.6, 42.3; 1000 71.6, 74.6,
+  //   73.1; 2000 138.6, 134.9, 130.0.  256 groups of 64 dims: 120 keys 7.5, 7.4, 10.3; 500 13.9, 8.8,
+  //   16.1; 1000 24.6, 13.3, 19.1.  16 groups of 128: 120 keys 7.2, 7.7, 10.2; 500 17.8, 9.3, 11.9;
+  //   1000 32.4, 14.6, 12.2.
+  const int tile_keys = f8 ? 64 : std::min(64, 8192 / (2 * D));
+  const long long keys = (long long)max_pages * page_size, tiles = (keys + tile_keys - 1) / tile_keys;
+  int gw = 0;
+  if (groups >= kWorkers) gw = keys <= 1024 ? 1 : 0;
+  else if (groups > kWorkers / 4) gw = tiles <= 8 ? 1 : 0;
+  else gw = tiles <= 2 ? 1 : tiles <= 16 ? 4 : 0;
+  auto launch = [&](auto* share, auto* one, auto* four) {
+    auto* kern = gw == 0 ? share : gw == 1 ? one : four;
+    return timed_launch(RA_KERNEL_DECODE, stream, [&] {
+      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : kWorkers), dim3(64 * (gw ? gw : 1)), 0, stream, a);
+      return hipGetLastError();
+    });
+  };
+  RA_HIP(D == 128 ? (f8 ? launch(paged_attn_kernel<128, true, 0>, paged_attn_kernel<128, true, 1>,
+                                 paged_attn_kernel<128, true, 4>)
+                        : launch(paged_attn_kernel<128, false, 0>, paged_attn_kernel<128, false, 1>,
+                                 paged_attn_kernel<128, false, 4>))
+                  : (f8 ? launch(paged_attn_kernel<64, true, 0>, paged_attn_kernel<64, true, 1>,
+                                 paged_attn_kernel<64, true, 4>)
+                        : launch(paged_attn_kernel<64, false, 0>, paged_attn_kernel<64, false, 1>,
+                                 paged_attn_kernel<64, false, 4>)));
+  if (gw) return RA_OK;
   // few groups: many parts each, a workgroup a slot; many: few parts, a wave a slot
   const bool few = groups <= 64;
   const dim3 grid(a.by_group ? (unsigned)groups : kWorkers, few ? M : (M + kJoinWaves - 1) / kJoinWaves);

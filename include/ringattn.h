@@ -421,6 +421,7 @@ int paged_plan(const int* lens, const int* n_new, const int* free_pages, const i
  *             whose slot lies outside the cache has q rotated and nothing stored.  Two rows with
  *             one slot leave elements of either in it.
  *   rotate    1: q and k are rotated by their positions (angles formed in double); 0: copied
+ * T < 2^24.
  */
 int paged_append(const void* q, const void* k, const void* v, void* q_out, void* k_pages, void* v_pages,
                  unsigned char* k_scales, unsigned char* v_scales, const int* slots, const int* positions, int T,

@@ -17,12 +17,13 @@ namespace {
 constexpr int kMxMaxT = 512;  // rows of one call
 
 // ---- packing -------------------------------------------------------------------------------
-// A thread a (group of 32 inputs, output); consecutive threads take consecutive outputs.  Scale:
+// A thread a (group of 32 inputs, output); consecutive threads take consecutive outputs, blockIdx.x
+// counts 256 of them and the groups (of whole blocks) together.  Scale:
 // the smallest power of two with which every element of the group is at most 6 in magnitude;
 // codes rounded to nearest, ties to the even code.
 __global__ __launch_bounds__(256) void mx4_pack_kernel(const bf16* w, uint8_t* w4, uint8_t* scales, int K, int N,
                                                        int kb) {
-  const int n = blockIdx.x * 256 + threadIdx.x, g = blockIdx.y;
+  const int g = blockIdx.x % (4 * kb), n = blockIdx.x / (4 * kb) * 256 + threadIdx.x;
   if (n >= (N + 15) / 16 * 16) return;
   const int k0 = 32 * g;
   float x[32];
@@ -178,7 +179,7 @@ extern "C" int mx4_pack(const void* w, void* w4, unsigned char* scales, int d_in
   if (int e = check_aligned({w, w4}, {scales})) return e;
   if (int e = check_mx(d_in, d_out)) return e;
   const int kb = (d_in + 127) / 128;
-  hipLaunchKernelGGL(mx4_pack_kernel, dim3((d_out + 255) / 256, 4 * kb), dim3(256), 0, stream, (const bf16*)w,
+  hipLaunchKernelGGL(mx4_pack_kernel, dim3((unsigned)((d_out + 255) / 256) * 4 * kb), dim3(256), 0, stream, (const bf16*)w,
                      (uint8_t*)w4, scales, d_in, d_out, kb);
   RA_HIP(hipGetLastError());
   return RA_OK;

@@ -368,6 +368,7 @@ extern "C" int paged_append(const void* q, const void* k, const void* v, void* q
   if (T <= 0 || Hq < 0 || (q && Hq == 0)) return set_err(RA_EINVAL, "sizes must be positive (T=%d Hq=%d)", T, Hq);
   if (int e = check_pages(page_size, n_pages, Hkv, D)) return e;
   if (D != 64 && D != 128) return set_err(RA_EUNSUPPORTED, "head dim D=%d not supported (64 or 128)", D);
+  if (T >= 1 << 24) return set_err(RA_EUNSUPPORTED, "T=%d rows exceeds 2^24-1", T);  // of 256 threads each
   if (!q) Hq = 0;
   if (Hq > kMaxHeads || Hkv > kMaxHeads)
     return set_err(RA_EUNSUPPORTED, "Hq=%d, Hkv=%d: at most %d heads", Hq, Hkv, kMaxHeads);

@@ -52,6 +52,7 @@ def test_append_refusals(lib):
     assert app(T=0) == RA_EINVAL and app(Hq=0) == RA_EINVAL and app(Hkv=0) == RA_EINVAL
     assert app(D=96, qs=768, kst=192, vst=192) == RA_EUNSUPPORTED
     assert app(page=48) == RA_EUNSUPPORTED
+    assert app(T=1 << 24) == RA_EUNSUPPORTED
     assert app(Hq=1025, qs=65600) == RA_EUNSUPPORTED
 
 

@@ -82,8 +82,8 @@ def check(s, o, lse, max_new=32):
     big_k = np.sqrt(np.nanmax(np.where(np.isfinite(s["ref"][0]), s["ref"][0], 0) ** 2, axis=(0, 1, 2)).sum())
     size = np.sqrt((q ** 2).sum(-1)) * big_k / math.sqrt(D)  # bounds the sum of a score's terms
     tol = (D * size + n + 64) * 2.0 ** -24
-    el = (np.abs(gl - lse_ref) - 4 * 2.0 ** -24 * np.abs(lse_ref))[fine]
-    eo = np.abs(go - o_ref)[fine]
+    el = np.abs(gl[fine] - lse_ref[fine]) - 4 * 2.0 ** -24 * np.abs(lse_ref[fine])
+    eo = np.abs(go[fine] - o_ref[fine])
     bound = (2.0 ** -8 * (np.abs(o_ref) + mag) * 1.01 + 2 * tol[..., None] * mag)[fine]
     log("  o %.2e of its bound, lse %.2e of %.2e" % ((eo / np.maximum(bound, 1e-30)).max(), el.max(), tol[fine].max()))
     assert (eo <= bound).all() and (el <= tol[fine]).all()
@@ -94,15 +94,19 @@ CASES = [  # lens, news, Hq, Hkv, D, page, pad
     ([33, 1, 0, 64, 65, 7], [1, 1, 0, 1, 1, 1], 8, 2, 128, 16, 3), ([0, 0, 5], [0, 0, 1], 2, 2, 64, 4, 0),
     ([1000, 3, 517], [1, 3, 32], 12, 4, 128, 64, 0), ([2049, 100], [8, 5], 28, 4, 128, 128, 2),
     ([700], [32], 32, 1, 64, 1024, 0), ([5000, 4999, 17], [1, 2, 17], 32, 8, 128, 16, 0),
-    ([300] * 40, [1] * 40, 16, 16, 64, 32, 0), ([3333], [3], 40, 8, 64, 2, 0), ([129, 64], [1, 1], 64, 1, 128, 8, 0)]
+    ([300] * 40, [1] * 40, 16, 16, 64, 32, 0), ([40, 9] * 36, [1, 2] * 36, 32, 16, 64, 16, 0),
+    ([70, 1, 0, 12] * 250, [1, 1, 0, 3] * 250, 3, 1, 128, 4, 1), ([260] * 3, [32, 1, 9], 80, 40, 64, 8, 0), ([3333], [3], 40, 8, 64, 2, 0), ([129, 64], [1, 1], 64, 1, 128, 8, 0)]
 
 
+# Tables as wide as the requests need (short ones are done in one launch), and wide enough for 70000
+# keys (shares of all tiles and a second launch).
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_attention(case, e4m3):
+def test_attention(case, e4m3, wide):
     lens, news, Hq, Hkv, D, page, pad = CASES[case]
-    log("paged attention %s e4m3=%d" % (CASES[case], e4m3))
-    s = make(case, lens, news, Hq, Hkv, D, page, e4m3, pad)
+    log("paged attention %s e4m3=%d wide=%d" % (CASES[case], e4m3, wide))
+    s = make(case, lens, news, Hq, Hkv, D, page, e4m3, pad, extra_cols=70000 // page if wide else 1)
     check(s, *call(s, max(max(news), 1)))
 
 
@@ -136,11 +140,12 @@ def test_bad_pages_in_the_middle_count_for_nothing(D, e4m3):
     check(s, *call(s, 4))
 
 
-def test_values_a_mask_hides_do_not_spread():
+@pytest.mark.parametrize("lens,cols", [((100, 260), 1), ((100, 260), 3000), ((30, 17), 1)])
+def test_values_a_mask_hides_do_not_spread(lens, cols):
     """Infinite and NaN keys and values of a later new token reach that token and those after it,
     no earlier one; of an ordinary token everybody."""
     for e4m3 in (False, True):
-        s = make(53, [100, 260], [6, 3], 8, 2, 128, 16, e4m3)
+        s = make(53, list(lens), [6, 3], 8, 2, 128, 16, e4m3, extra_cols=cols)
 
         def put(r, p, h, what):
             i = s["table_np"][r, p // 16]
@@ -150,8 +155,8 @@ def test_values_a_mask_hides_do_not_spread():
                 else:
                     s[t][i, p % 16, h, 5] = float(what)
 
-        put(0, 97, 1, "nan")   # the fourth new token of request 0, key head 1
-        put(1, 259, 0, "inf")  # the last of request 1, key head 0
+        put(0, lens[0] - 3, 1, "nan")  # the fourth new token of request 0, key head 1
+        put(1, lens[1] - 1, 0, "inf")  # the last of request 1, key head 0
         o, lse = call(s, 6)
         go = np64(o)
         assert np.isnan(go[3:6, 4:]).all() and np.isfinite(go[:3]).all() and np.isfinite(go[3:6, :4]).all()
@@ -163,9 +168,10 @@ def test_values_a_mask_hides_do_not_spread():
             assert (np.abs(go - ref) <= 2.0 ** -8 * 1.01 * (np.abs(ref) + mag) + 1e-4 * mag)[rows].all()
 
 
-def test_scores_of_minus_infinity_and_nan():
+@pytest.mark.parametrize("cols", [1, 5000])
+def test_scores_of_minus_infinity_and_nan(cols):
     """-inf scores weigh nothing; a row of nothing else has o = 0, lse = -inf; NaN spreads."""
-    s = make(54, [50, 40], [1, 1], 2, 1, 64, 16, False)
+    s = make(54, [50, 40], [1, 1], 2, 1, 64, 16, False, extra_cols=cols)
     s["q"][:] = 1.0
     for r, keys in ((0, range(10)), (1, range(40))):
         for p in keys:

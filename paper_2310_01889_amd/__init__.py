@@ -469,19 +469,19 @@ def paged_plan(lens, n_new, free_pages, free_head, block_table, cu_rows, new_len
     """int32 tensors: lens, n_new, new_lens [R], free_pages [n_free], free_head [1] or None,
     block_table [R, max_pages], cu_rows [R + 1], slots, positions [T], counts [4]."""
     R, max_pages = block_table.shape
-    T, (dev, st) = len(slots), _current(stream)
+    T, (dev, st) = slots.numel(), _current(stream)
     _call("paged_plan", _ints(lens, "lens", R, dev), _ints(n_new, "n_new", R, dev),
-          _ints(free_pages, "free_pages", len(free_pages), dev), _ints(free_head, "free_head", 1, dev),
+          _ints(free_pages, "free_pages", free_pages.numel(), dev), _ints(free_head, "free_head", 1, dev),
           _arg(block_table, "block_table", _I32, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
           _ints(new_lens, "new_lens", R, dev), _ints(slots, "slots", T, dev),
           _ints(positions, "positions", T, dev), _ints(counts, "counts", 4, dev), R, page_size,
-          max_pages, n_pages, len(free_pages), T, st)
+          max_pages, n_pages, free_pages.numel(), T, st)
 
 
 def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=None, v_scales=None, rotate=True,
                  stream=None):
     """q [T, Hq, D] (or None, with q_out), k, v [T, Hkv, D]: rows may be strided."""
-    T, (dev, st) = len(slots), _current(stream)
+    T, (dev, st) = slots.numel(), _current(stream)
     kp, vp, ks, vs, kind, (n_pages, page_size, Hkv, D) = _cache(k_pages, v_pages, k_scales, v_scales, dev)
     Hq = 0 if q is None else q.shape[1]
     q_at, q_row = (None, 0) if q is None else _rows(q, "q", T, Hq, D, dev)

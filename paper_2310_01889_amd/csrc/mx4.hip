@@ -127,9 +127,7 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
       e[j] = *(const uint32_t*)(sc[j] + (long long)b * 64);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (128 * b + 32 * s >= a.K) break;
+    auto product = [&](int s) __attribute__((always_inline)) {  // of 32 inputs
       bf16x8 x[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n) x[n] = *(const bf16x8*)(slab + n * 4096 + (xoff ^ (64 * s)));
@@ -139,6 +137,17 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[j][n] = mfma16(wv, x[n], acc[j][n]);
       }
+    };
+    if (128 * (b + 1) <= a.K) {  // (branches between the steps would keep their reads apart)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        if (NT * NB >= 16 && s == 2) __builtin_amdgcn_sched_barrier(0);  // not all reads at once: registers
+        product(s);
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 3; ++s)
+        if (128 * b + 32 * s < a.K) product(s);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slab has been read
   }

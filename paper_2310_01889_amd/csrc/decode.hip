@@ -37,14 +37,6 @@ struct DecodeArgs {
   float scale;
 };
 
-// The bf16 numbers next below two non-negative floats (of zero: zero), a in the low half.  What
-// they leave of a number above zero is then above zero as well.
-__device__ __forceinline__ uint32_t bf16x2_below(float a, float b) {
-  const uint32_t x = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, a), 1u);
-  const uint32_t y = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, b), 1u);
-  return __builtin_amdgcn_perm(y, x, 0x07060302u);
-}
-
 // One wave: the partial state of all Tq queries (lane l % 32 = query slot) over the kch
 // keys of one chunk.  The arithmetic per 32-key tile is that of the forward step kernel:
 // S^T = K Q^T on the matrix cores (K rows from LDS with bits 2 and 3 of the row index

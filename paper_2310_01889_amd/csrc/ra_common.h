@@ -105,6 +105,14 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
+// The bf16 numbers next below two non-negative floats (of zero: zero), a in the low half.  What
+// they leave of a number above zero is then above zero as well.
+__device__ __forceinline__ uint32_t bf16x2_below(float a, float b) {
+  const uint32_t x = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, a), 1u);
+  const uint32_t y = __builtin_elementwise_sub_sat(__builtin_bit_cast(uint32_t, b), 1u);
+  return __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+
 // Map a linear workgroup id so that each XCD (workgroups are dispatched round-robin
 // over the 8 XCDs) receives a contiguous range of logical tiles: tiles that share
 // key/value data then share one L2.

@@ -28,8 +28,23 @@ namespace {
 
 constexpr int kMaxNew = 32;      // new tokens a request
 constexpr int kSlots = 32;       // query slots a wave
-constexpr int kWorkers = 1024;   // waves: one a SIMD (four tile pairs of 32 KB a compute unit)
 constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
+
+// Keys a tile, and the waves that share all tiles.
+// bf16: tiles of 8 KB, four of them (32 KB of LDS) a wave.  256-byte rows: three waves a compute unit
+// are enough in flight, a fourth only lengthens the queues at the memory (262144 tokens of 32 heads 697
+// us with 768 waves, 747 with 1024, 766 with 896, which leaves some units more than others; a batch of
+// 64 195 and 202; 512 waves 937).  128-byte rows: four (24 requests of 700 to 16001 tokens, 8 heads: 95 us
+// with three, 90 with four).
+// 8 bits: rows have half the bytes and the same products: 4 KB tiles, so that a SIMD's second wave
+// converts and multiplies while the first one waits; six waves a compute unit (those 24 requests,
+// 128 dims: 112 us with 1024 waves, 97 with 1536, 106 with 2048; up to eight tokens a request 126, 107
+// and 113; tiles of 8 KB with 1024 117 and 116).
+// Four waves that join in LDS take 64 keys at a time in 8 bits as well, which is the room their states
+// need.
+constexpr int kMaxWorkers = 1536;
+constexpr int workers(int D, bool f8) { return f8 ? 1536 : D == 128 ? 768 : 1024; }
+constexpr int tile_keys(int D, bool f8, int gw) { return D == 64 || (f8 && gw > 1) ? 64 : 32; }
 
 // What the second launch joins: the parts of a group of units (request, key head, round) that
 // several waves share, written by the first of them.  parts = 0: nothing to join.
@@ -56,7 +71,7 @@ struct PagedArgs {
   int M;            // query slots of a group at most
   int rounds;       // rounds of slots of a request at most
   int by_group;     // entries of split: 1 a group, 0 a wave
-  int teams;        // kWorkers / Hkv
+  int teams;        // workers / Hkv
   float scale;
 };
 
@@ -146,7 +161,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : 1), GW > 1 ? 1 : 2) void paged_attn
   constexpr int NW = GW ? GW : 1;
   constexpr int RB = F8 ? D : 2 * D;              // bytes a row
   constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
-  constexpr int KT = 8192 / RB < 64 ? 8192 / RB : 64;  // keys a tile
+  constexpr int KT = tile_keys(D, F8, GW);        // keys a tile
   constexpr int LOADS = KT / RPL, NS = KT / 32, NKK = D / 16, NDT = D / 32;
   constexpr int TB = KT * RB;                     // bytes of a tile; its scales: a dword a key
   __shared__ __attribute__((aligned(1024))) uint8_t s_tiles[NW][2][2][TB];  // wave, K or V, buffer
@@ -689,7 +704,7 @@ extern "C" int paged_attn_workspace(int R, int Hq, int Hkv, int D, int max_new, 
   g_err.clear();
   if (!bytes) return set_err(RA_EINVAL, "null pointer argument");
   if (int e = paged_check_heads(R, Hq, Hkv, D, max_new)) return e;
-  *bytes = paged_bytes(kWorkers, paged_slots(Hq, Hkv, max_new), D);
+  *bytes = paged_bytes(kMaxWorkers, paged_slots(Hq, Hkv, max_new), D);
   return RA_OK;
 }
 
@@ -706,7 +721,9 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   const bool f8 = kv_type == RA_KV_E4M3;
   const int M = paged_slots(Hq, Hkv, max_new);
   const int rounds = (int)(((long long)max_new * (Hq / Hkv) + kSlots - 1) / kSlots);
-  const size_t need = paged_bytes(kWorkers, M, D);
+  const size_t need = paged_bytes(kMaxWorkers, M, D);
+  const int nw = std::max(workers(D, f8), Hkv);  // a team at least
+  static_assert(kMaxWorkers >= kMaxHeads);
   if (workspace && workspace_bytes < need)
     return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   CallResources res(stream);
@@ -716,10 +733,10 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   }
   const long long groups = (long long)R * Hkv * rounds;
   float* acc = (float*)workspace;
-  float* ml = acc + (size_t)kWorkers * 2 * M * D;
+  float* ml = acc + (size_t)nw * 2 * M * D;
   PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, acc, ml,
-              (Split*)(ml + (size_t)kWorkers * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
-              groups <= kWorkers, kWorkers / Hkv, 1.f / sqrtf((float)D)};
+              (Split*)(ml + (size_t)nw * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
+              groups <= nw, nw / Hkv, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (8 KB of keys, 64 keys at most) are few, four waves
@@ -729,16 +746,15 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   //   73.1; 2000 138.6, 134.9, 130.0.  256 groups of 64 dims: 120 keys 7.5, 7.4, 10.3; 500 13.9, 8.8,
   //   16.1; 1000 24.6, 13.3, 19.1.  16 groups of 128: 120 keys 7.2, 7.7, 10.2; 500 17.8, 9.3, 11.9;
   //   1000 32.4, 14.6, 12.2.
-  const int tile_keys = f8 ? 64 : std::min(64, 8192 / (2 * D));
-  const long long keys = (long long)max_pages * page_size, tiles = (keys + tile_keys - 1) / tile_keys;
+  const long long keys = (long long)max_pages * page_size, kt = f8 || D == 64 ? 64 : 32, tiles = (keys + kt - 1) / kt;
   int gw = 0;
-  if (groups >= kWorkers) gw = keys <= 1024 ? 1 : 0;
-  else if (groups > kWorkers / 4) gw = tiles <= 8 ? 1 : 0;
+  if (groups >= 1024) gw = keys <= 1024 ? 1 : 0;
+  else if (groups > 256) gw = tiles <= 8 ? 1 : 0;
   else gw = tiles <= 2 ? 1 : tiles <= 16 ? 4 : 0;
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {
-      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : kWorkers), dim3(64 * (gw ? gw : 1)), 0, stream, a);
+      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : nw), dim3(64 * (gw ? gw : 1)), 0, stream, a);
       return hipGetLastError();
     });
   };
@@ -753,7 +769,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   if (gw) return RA_OK;
   // few groups: many parts each, a workgroup a slot; many: few parts, a wave a slot
   const bool few = groups <= 64;
-  const dim3 grid(a.by_group ? (unsigned)groups : kWorkers, few ? M : (M + kJoinWaves - 1) / kJoinWaves);
+  const dim3 grid(a.by_group ? (unsigned)groups : nw, few ? M : (M + kJoinWaves - 1) / kJoinWaves);
   auto* join = D == 128 ? (few ? paged_join_kernel<128, kJoinWaves> : paged_join_kernel<128, 1>)
                         : (few ? paged_join_kernel<64, kJoinWaves> : paged_join_kernel<64, 1>);
   hipLaunchKernelGGL(join, grid, dim3(64 * kJoinWaves), 0, stream, a);

@@ -237,3 +237,13 @@ def test_workspace_streams_and_repeats():
         ra.paged_attn_decode(s["q"], s["k"], s["v"], s["table"], s["lens"][:2], s["cu"], o, lse, 8)
     with pytest.raises(TypeError):
         ra.paged_attn_decode(s["q"], s["k"].half(), s["v"].half(), s["table"], s["lens"], s["cu"], o, lse, 8)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_heads_than_waves_a_team(D, e4m3):
+    """As many key heads as the library takes: one team of waves for all requests."""
+    s = make(60 + D, [70, 3, 0, 41], [2, 1, 0, 3], 1024, 1024, D, 8, e4m3, extra_cols=9000)
+    check(s, *call(s, 3))
+    s = make(61 + D, [90, 20], [1, 1], 900, 900, D, 16, e4m3, extra_cols=9000)
+    check(s, *call(s, 1))

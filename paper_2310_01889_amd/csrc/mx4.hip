@@ -4,6 +4,7 @@
 // y [T, d_out] = x [T, d_in] W (+ residual).  The weights lie in blocks of 16 outputs x 128
 // inputs, 1 KB of codes each: lane l of a wave loads 16 bytes, output l % 16, whose bytes
 // 4s .. 4s + 3 are the 8 inputs 32 s + 8 (l / 16) ..., the A operand of one 16x16x32 product.
+#include <limits.h>
 #include <math.h>
 
 #include "ra_common.h"
@@ -76,27 +77,32 @@ __device__ __forceinline__ bf16x8 from_e2m1(uint32_t codes, float scale) {
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// A workgroup of WV waves takes NB blocks of 16 outputs for NT tiles of 16 rows; its waves take
-// turns along the inputs, 128 at a time, and their sums are added in wave order through LDS.
-// Every weight is read once for NT tiles, straight from memory into the lane that needs it, and
-// becomes a bf16 operand once.  The rows' 128 inputs go through a slab of LDS of the wave's own:
-// an operand's neighbouring lanes are neighbouring rows, and a load of 64 lanes from 16 rows
-// takes the address unit four times as long as the slab's loads of whole 256-byte pieces (48 x
-// 11008 x 4096: 33 us without the slab, 16 with it; 7 x 4096 x 11008: 9 and 7).  Workgroups start
-// at different inputs: the rows' pieces at one place lie in few channels of the L2 where the row
-// length is a multiple of 4 KB (32 x 4096 x 4096: 7.6 us without, 6.7).
-// Bound by latency for few weights; by the weights' bytes and, for many rows, by x, which every
-// workgroup reads whole from L2.
-template <int NT, int NB, int WV>
+// A workgroup of WV waves takes NB blocks of 16 outputs for NT tiles of 16 rows (of one tile: for 4 XL
+// rows); its waves take turns along the inputs, 128 at a time, and their sums are added in wave order
+// through LDS.  Every weight becomes a bf16 operand once.  The rows' 128 inputs go through a slab of
+// LDS of the wave's own: an operand's neighbouring lanes are neighbouring rows, and a load of 64 lanes
+// from 16 rows takes the address unit four times as long as the slab's loads of whole 256-byte
+// pieces (48 x 11008 x 4096: 33 us without the slab, 16 with it; 7 x 4096 x 11008: 9 and 7).
+// PIPE: codes and scales go through LDS as well and a wave has two stages, one in flight while the
+// other is computed; else weights go straight to registers and other waves hide the loads, eight
+// of them where their slabs are large (64 x 4096 x 4096 in 2 x 2 tiles: 6.7 us with two stages, 7.8 with
+// one; 24 x 4096 x 11008 in 2 x 4: 11.3 and 10.9).
+// Workgroups start at different inputs: the rows' pieces at one place lie in few channels of the L2
+// where the row length is a multiple of 4 KB (32 x 4096 x 4096: 7.6 us without, 6.7).
+// Bound by latency for few weights; by the weights' bytes; for many rows by what the compute units
+// take from L2, about 60 bytes a ns each, x being read whole by every column of workgroups.
+template <int NT, int NB, int WV, bool PIPE, int XL = 4 * NT>
 __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
-  constexpr int SLAB = NT * 4096, SUMS = NT * NB * 1024;
-  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[WV][SLAB > SUMS ? SLAB : SUMS];
+  constexpr int SLAB = XL * 1024, STAGE = SLAB + (PIPE ? NB * 1280 : 0), LOADS = XL + 2 * NB;
+  constexpr int SUMS = NT * NB * 1024, MEM = PIPE ? 2 * STAGE : STAGE;
+  __shared__ __attribute__((aligned(1024))) uint8_t s_mem[WV][MEM > SUMS ? MEM : SUMS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, c = lane >> 4;
   const int nb = (a.N + 15) / 16, i0 = blockIdx.x * NB, t0 = blockIdx.y * NT * 16;
   const int rows = min(NT * 16, a.T - t0);
   uint8_t* slab = s_mem[wave];
-  const int xoff = l16 * 256 + 16 * (c ^ swz<128>(l16));
+  const int xr = XL < 4 ? l16 % (4 * XL) : l16;  // (rows past the last are others again; nothing uses them)
+  const int xoff = xr * 256 + 16 * (c ^ swz<128>(xr));
   const int start = (int)(blockIdx.x * 7u % (unsigned)a.kb);
   const uint8_t *w4[NB], *sc[NB];
 #pragma unroll
@@ -105,32 +111,62 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
     w4[j] = a.w4 + (long long)i * a.kb * 1024 + lane * 16;
     sc[j] = a.scales + (long long)i * a.kb * 64 + l16 * 4;
   }
+  auto block_of = [&](int at) { return at + start < a.kb ? at + start : at + start - a.kb; };
+  auto load = [&](int at, uint8_t* to) __attribute__((always_inline)) {
+    const int b = block_of(at);
+    if constexpr (PIPE) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        dma_lds16_at(w4[j] + (long long)b * 1024, lds_addr(to) + SLAB + j * 1280);
+        dma_lds4_at(sc[j] + (long long)b * 64, lds_addr(to) + SLAB + j * 1280 + 1024);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < XL; ++j) {
+      if (!PIPE && 4 * j >= rows) break;  // (PIPE counts its loads)
+      // four rows a load; rows and inputs past the ends read others, which nothing uses
+      const int r = 4 * j + c, k = min(128 * b + 8 * (l16 ^ swz<128>(r)), a.K - 8);
+      dma_lds16_at(a.x + (long long)min(t0 + r, a.T - 1) * a.K + k, lds_addr(to) + j * 1024);
+    }
+  };
   f32x4 acc[NB][NT];
 #pragma unroll
   for (int j = 0; j < NB; ++j)
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[j][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int at = wave; at < a.kb; at += WV) {
-    const int b = at + start < a.kb ? at + start : at + start - a.kb;
-#pragma unroll
-    for (int j = 0; j < NT * 4; ++j) {
-      if (4 * j >= rows) break;
-      // four rows a load; rows and inputs past the ends read others, which nothing uses
-      const int r = 4 * j + c, k = min(128 * b + 8 * (l16 ^ swz<128>(r)), a.K - 8);
-      dma_lds16_at(a.x + (long long)min(t0 + r, a.T - 1) * a.K + k, lds_addr(slab) + j * 1024);
-    }
+  if (PIPE && wave < a.kb) load(wave, slab);
+#pragma unroll 1
+  for (int at = wave, st = 0; at < a.kb; at += WV, st ^= 1) {
+    const int b = block_of(at);
+    uint8_t* here = slab + (PIPE ? st * STAGE : 0);
     u32x4 w[NB];
     uint32_t e[NB];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // what is loaded into has been read
+    if constexpr (PIPE) {
+      if (at + WV < a.kb) {
+        load(at + WV, slab + (st ^ 1) * STAGE);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");  // this stage has landed
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      w[j] = *(const u32x4*)(w4[j] + (long long)b * 1024);
-      e[j] = *(const uint32_t*)(sc[j] + (long long)b * 64);
+      for (int j = 0; j < NB; ++j) {
+        w[j] = *(const u32x4*)(here + SLAB + j * 1280 + lane * 16);
+        e[j] = *(const uint32_t*)(here + SLAB + j * 1280 + 1024 + lane * 4);
+      }
+    } else {
+      load(at, slab);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        w[j] = *(const u32x4*)(w4[j] + (long long)b * 1024);
+        e[j] = *(const uint32_t*)(sc[j] + (long long)b * 64);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     auto product = [&](int s) __attribute__((always_inline)) {  // of 32 inputs
       bf16x8 x[NT];
 #pragma unroll
-      for (int n = 0; n < NT; ++n) x[n] = *(const bf16x8*)(slab + n * 4096 + (xoff ^ (64 * s)));
+      for (int n = 0; n < NT; ++n) x[n] = *(const bf16x8*)(here + n * 4096 + (xoff ^ (64 * s)));
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
         const bf16x8 wv = from_e2m1(w[j][s], __uint_as_float((e[j] >> (8 * s) & 255u) << 23));
@@ -149,8 +185,8 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
       for (int s = 0; s < 3; ++s)
         if (128 * b + 32 * s < a.K) product(s);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slab has been read
   }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slab has been read
 #pragma unroll
   for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -204,28 +240,46 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
   if (T > kMxMaxT) return set_err(RA_EUNSUPPORTED, "T=%d exceeds %d rows", T, kMxMaxT);
   MxArgs a{(const bf16*)x, (const uint8_t*)w4, scales, (const bf16*)residual, (bf16*)y, T, d_in, d_out,
            (d_in + 127) / 128};
-  // NT: a pass over the weights for up to 64 rows.  Blocks a workgroup: as many as leave one
-  // workgroup a compute unit (of 256), for then x is read least often.  us with one, two, four
-  // blocks: 64 x 4096 x 11008 (688 blocks) -, 19.3, 15.4; 20 x 2048 x 6000 (375) 5.9, 5.2, 6.2; 32 x
-  // 4096 x 4096 (256) 6.7, 7.3, 8.3.  For one tile x is little: one block, with 16 waves where the
-  // blocks are no more than the compute units (1 x 11008 x 4096: 6.4 us, 8 waves 8.3; 7 x 4096 x
-  // 11008, 688 blocks: 8.4, 8 waves 6.9).
+  // Tiles NT and blocks NB a workgroup: the pair with which a compute unit (of 256) takes the fewest
+  // bytes, counting for every input 8 of x for four rows and 17 a block of weights, twice what
+  // they are, for they come from memory and not from L2.  us of the pairs 1x1, 1x2, 1x4, 2x2, 2x4, 3x4:
+  //   32 x 4096 x 4096   7.5  5.2  6.8  6.7  -     -        20 x 4096 x 2048   4.6  4.9  6.6  6.2  -  -
+  //   48 x 11008 x 4096  20.6 18.6 15.6 15.6 20.6  -        48 x 4096 x 11008  -  15.8 17.2 16.9 16.5 13.2
+  //   96 x 4096 x 11008  -    25.9 25.3 24.5 20.6  21.0
+  // 4x4 for 64 x 4096 x 11008: 16.8 us, 2x4 17.9.  NB = 4 with several tiles, one stage: eight waves where
+  // every workgroup has a compute unit of its own (24 x 4096 x 11008 10.9 us, four waves 15.4), else four,
+  // two workgroups a unit (300 x 4096 x 4096 18.3, eight waves 20.6).  1x1 and up to eight rows: 16 waves
+  // in the first case (1 x 11008 x 4096 6.6 us, eight waves 8.1).
   const int tiles = (T + 15) / 16, blocks = (d_out + 15) / 16;
-  auto run = [&](auto kernel, int nt, int nb, int wv) {
+  const int xl = T <= 4 ? 1 : T <= 8 ? 2 : 4;
+  auto groups = [&](int nt, int nb) { return (long long)((blocks + nb - 1) / nb) * ((tiles + nt - 1) / nt); };
+  static constexpr int kPairs[][2] = {{4, 4}, {3, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}, {1, 1}};
+  int nt = 1, nb = 1;
+  long long least = LLONG_MAX;
+  for (const auto& p : kPairs) {
+    if (p[0] > tiles) continue;
+    const long long cost = (groups(p[0], p[1]) + 255) / 256 * (8 * (p[0] == 1 ? xl : 4 * p[0]) + 17 * p[1]);
+    if (cost < least) least = cost, nt = p[0], nb = p[1];
+  }
+  const bool wide = groups(nt, nb) <= 256;
+  auto run = [&](auto* kernel, int wv) {
     hipLaunchKernelGGL(kernel, dim3((blocks + nb - 1) / nb, (tiles + nt - 1) / nt), dim3(64 * wv), 0, stream, a);
   };
-  const int nb = blocks <= 256 ? 1 : blocks <= 512 ? 2 : 4;
-  if (tiles == 1 && nb == 1) run(mx4_linear_kernel<1, 1, 16>, 1, 1, 16);
-  else if (tiles == 1) run(mx4_linear_kernel<1, 1, 8>, 1, 1, 8);
-  else if (tiles == 2 && nb == 1) run(mx4_linear_kernel<2, 1, 8>, 2, 1, 8);
-  else if (tiles == 2 && nb == 2) run(mx4_linear_kernel<2, 2, 8>, 2, 2, 8);
-  else if (tiles == 2) run(mx4_linear_kernel<2, 4, 8>, 2, 4, 8);
-  else if (tiles == 3 && nb == 1) run(mx4_linear_kernel<3, 1, 8>, 3, 1, 8);
-  else if (tiles == 3 && nb == 2) run(mx4_linear_kernel<3, 2, 8>, 3, 2, 8);
-  else if (tiles == 3) run(mx4_linear_kernel<3, 4, 8>, 3, 4, 8);
-  else if (nb == 1) run(mx4_linear_kernel<4, 1, 8>, 4, 1, 8);
-  else if (nb == 2) run(mx4_linear_kernel<4, 2, 8>, 4, 2, 8);
-  else run(mx4_linear_kernel<4, 4, 8>, 4, 4, 8);
+  auto one_tile = [&](auto* four, auto* eight, auto* sixteen) { run(xl == 1 ? four : xl == 2 ? eight : sixteen, 8); };
+  if (nt == 1 && nb == 1 && wide && xl < 4)
+    run(xl == 1 ? mx4_linear_kernel<1, 1, 16, true, 1> : mx4_linear_kernel<1, 1, 16, true, 2>, 16);
+  else if (nt == 1 && nb == 1)
+    one_tile(mx4_linear_kernel<1, 1, 8, true, 1>, mx4_linear_kernel<1, 1, 8, true, 2>, mx4_linear_kernel<1, 1, 8, true>);
+  else if (nt == 1 && nb == 2)
+    one_tile(mx4_linear_kernel<1, 2, 8, true, 1>, mx4_linear_kernel<1, 2, 8, true, 2>, mx4_linear_kernel<1, 2, 8, true>);
+  else if (nt == 1)
+    one_tile(mx4_linear_kernel<1, 4, 8, true, 1>, mx4_linear_kernel<1, 4, 8, true, 2>, mx4_linear_kernel<1, 4, 8, true>);
+  else if (nt == 2 && nb == 2) run(mx4_linear_kernel<2, 2, 7, true>, 7);
+  else if (nt == 2 && wide) run(mx4_linear_kernel<2, 4, 8, false>, 8);
+  else if (nt == 2) run(mx4_linear_kernel<2, 4, 4, false>, 4);
+  else if (nt == 3 && wide) run(mx4_linear_kernel<3, 4, 8, false>, 8);
+  else if (nt == 3) run(mx4_linear_kernel<3, 4, 4, false>, 4);
+  else run(mx4_linear_kernel<4, 4, 8, false>, 8);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

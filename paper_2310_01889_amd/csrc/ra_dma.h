@@ -31,6 +31,9 @@ __device__ __forceinline__ void dma_lds4(const __amdgpu_buffer_rsrc_t& rsrc, uns
 __device__ __forceinline__ void dma_lds16_at(const void* addr, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
 }
+__device__ __forceinline__ void dma_lds4_at(const void* addr, unsigned lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
+}
 __device__ __forceinline__ void dma_lds1_at(const void* addr, unsigned lds_addr) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_ubyte %1, off" ::"s"(lds_addr), "v"(addr) : "memory");
 }

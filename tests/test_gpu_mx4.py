@@ -63,6 +63,33 @@ def test_linear(T, K, N, residual):
     assert (err <= bound).all() and (guard[T * N:] == 7).all()
 
 
+@pytest.mark.parametrize("T,K,N", [
+    (1, 2208, 9005), (1, 2208, 4100), (2, 1184, 14000), (5, 1184, 20000), (7, 2208, 5003), (8, 1184, 11000),
+    (9, 4256, 1000), (12, 1184, 20000), (16, 2208, 8190), (11, 2208, 9005), (20, 2208, 6001), (20, 416, 20000),
+    (31, 1184, 11000), (70, 416, 9005), (40, 1184, 12001), (90, 1056, 11000), (60, 1184, 9005), (200, 416, 8190)])
+def test_linear_in_every_shape_of_workgroup(T, K, N):
+    """Rows and outputs that take each number of row tiles and output blocks a workgroup, with a
+    ragged end each; more inputs than the waves of one take at a time."""
+    log("mx4 linear T=%d K=%d N=%d" % (T, K, N))
+    g = torch.Generator(device="cuda").manual_seed(T + K + N)
+    w4, scales = ra.mx4_weights((0.02 * torch.randn(K, N, generator=g, device="cuda")).to(torch.bfloat16))
+    x = torch.randn(T, K, generator=g, device="cuda").to(torch.bfloat16)
+    res = torch.randn(T, N, generator=g, device="cuda").to(torch.bfloat16)
+    guard = torch.full((T * N + 8,), 7.0, dtype=torch.bfloat16, device="cuda")
+    y = guard[:T * N].view(T, N)
+    ra.mx4_linear(x, w4, scales, res, y)
+    torch.cuda.synchronize()
+    wv = OS.mx4_values(w4.cpu().numpy(), scales.cpu().numpy(), K, N)
+    ref = np64(x) @ wv + np64(res)
+    size = np.abs(np64(x)) @ np.abs(wv) + np.abs(np64(res))
+    err, bound = np.abs(np64(y) - ref), 2.0 ** -8 * np.abs(ref) + (K + 1) * 2.0 ** -24 * size
+    log("  %.2e of its bound" % (err / bound).max())
+    assert (err <= bound).all() and (guard[T * N:] == 7).all()
+    again = torch.empty_like(y)
+    ra.mx4_linear(x, w4, scales, res, again)
+    assert torch.equal(y, again)
+
+
 def test_every_code_and_scale():
     """Each of the 16 codes under scales from 2^-126 to 2^127, and a NaN scale, read by a product
     that picks one input out."""

@@ -74,3 +74,23 @@ def test_plan_bad_integers():
     table = np.array([[0, -1, -1, -1], [99, 2, -1, -1], [3, -9, 4, -1], [-1] * 4, [5, 6, 7, 8]])
     _check([3, 6, 9, -4, big], [2, 1, 1, 3, 2], [11, 200, -1, 9], None, table, 4, 12, 16)
     _check([3, 6, 9, 0, 0], [big, -1, big, big, 0], [11, 200, -1, 9], 0, table, 4, 12, 5)
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_slots_and_positions_off_a_16_byte_boundary(shift):
+    lens, n_new, page, T = np.array([5, 0, 17, 40]), np.array([3, 9, 0, 6]), 8, 23
+    free, table = np.arange(30, 60), np.arange(24).reshape(4, 6)
+    want = OS.plan(lens, n_new, free, 0, table, page, 64, T)
+    buf = torch.full((2, T + 8), -77, dtype=torch.int32, device="cuda")
+    slots, pos = buf[0, shift:shift + T], buf[1, shift:shift + T]
+    td, cu, nl, counts = _i32(table), _i32([0] * 5), _i32([0] * 4), _i32([0] * 4)
+    ra.paged_plan(_i32(lens), _i32(n_new), _i32(free), None, td, cu, nl, slots, pos, counts, page, 64)
+    assert np.array_equal(slots.cpu().numpy(), want[3]) and np.array_equal(pos.cpu().numpy(), want[4])
+    assert (buf[:, :shift] == -77).all() and (buf[:, shift + T:] == -77).all()
+
+
+def test_positions_past_31_bits():
+    """Positions end at 2^31 - 1; slots go by what they would be."""
+    page, cols = 1024, (1 << 21) + 2
+    table = np.full((1, cols), 3)
+    _check(np.array([2 ** 31 - 2]), np.array([1027]), np.array([7, 5]), None, table, page, 9, 1030)

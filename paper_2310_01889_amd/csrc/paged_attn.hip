@@ -30,20 +30,21 @@ constexpr int kMaxNew = 32;      // new tokens a request
 constexpr int kSlots = 32;       // query slots a wave
 constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
 
-// Keys a tile, and the waves that share all tiles.
-// bf16: tiles of 8 KB, four of them (32 KB of LDS) a wave.  256-byte rows: three waves a compute unit
-// are enough in flight, a fourth only lengthens the queues at the memory (262144 tokens of 32 heads 697
-// us with 768 waves, 747 with 1024, 766 with 896, which leaves some units more than others; a batch of
-// 64 195 and 202; 512 waves 937).  128-byte rows: four (24 requests of 700 to 16001 tokens, 8 heads: 95 us
-// with three, 90 with four).
+// Keys a tile, and the waves that share all tiles, four a workgroup: neighbouring key heads read pieces of
+// one token, so their waves stay close to one another in time and place (24 requests of 700 to 16001
+// tokens, us with one, two and four waves a workgroup: 8 heads of 128 dims in bf16 160-182, 152-156,
+// 152-154; 16 heads of 64 dims 168-180, 155-161, 152-157; 32 heads in 8 bits 346, 310, 294).
+// bf16: tiles of 8 KB, four of them (32 KB of LDS) a wave, four waves a compute unit (768 waves in
+// place of 1024: 163 us for 153; 262144 tokens of 32 heads 738 for 713).
 // 8 bits: rows have half the bytes and the same products: 4 KB tiles, so that a SIMD's second wave
-// converts and multiplies while the first one waits; six waves a compute unit (those 24 requests,
-// 128 dims: 112 us with 1024 waves, 97 with 1536, 106 with 2048; up to eight tokens a request 126, 107
-// and 113; tiles of 8 KB with 1024 117 and 116).
+// converts and multiplies while the first one waits (8 KB tiles and 1024 waves: 117 us for 98).
+// Seven waves a compute unit for 128 dims, whose partial states stay below 64 MB, eight for 64 (us
+// with 1280, 1536, 1792, 2048 waves: 8 heads of 128 106, 95, 91, 92; of 64 78, 71, 66, 62).
 // Four waves that join in LDS take 64 keys at a time in 8 bits as well, which is the room their states
 // need.
-constexpr int kMaxWorkers = 1536;
-constexpr int workers(int D, bool f8) { return f8 ? 1536 : D == 128 ? 768 : 1024; }
+constexpr int kShareWaves = 4;
+constexpr int workers(int D, bool f8) { return !f8 ? 1024 : D == 128 ? 1792 : 2048; }
+constexpr int max_workers(int D) { return workers(D, true); }
 constexpr int tile_keys(int D, bool f8, int gw) { return D == 64 || (f8 && gw > 1) ? 64 : 32; }
 
 // What the second launch joins: the parts of a group of units (request, key head, round) that
@@ -147,7 +148,7 @@ __device__ __forceinline__ u32x4 only_finite(u32x4 x) {
   return x;
 }
 
-// GW = 0: one wave a workgroup, its team's share of all units.  GW > 0: short requests; GW waves take
+// GW = 0: each wave its team's share of all units.  GW > 0: short requests; GW waves take
 // the tiles of one group (request, key head, round) in turns and join their states in LDS, so that
 // one launch does.  Per tile the arithmetic of the decode kernel over a contiguous cache:
 // S^T = K Q^T on the matrix cores (K rows with bits 2 and 3 of the row index swapped as the A
@@ -157,15 +158,15 @@ __device__ __forceinline__ u32x4 only_finite(u32x4 x) {
 // 8-bit tiles become bf16 operands in registers, exactly: key rows under their scales, values as
 // they are, their scales (powers of two) going into the probabilities before those are rounded.
 template <int D, bool F8, int GW>
-__global__ __launch_bounds__(64 * (GW ? GW : 1), GW > 1 ? 1 : 2) void paged_attn_kernel(const PagedArgs a) {
-  constexpr int NW = GW ? GW : 1;
+__global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void paged_attn_kernel(const PagedArgs a) {
+  constexpr int NW = GW ? GW : 1, WAVES = GW ? GW : kShareWaves;  // waves of a group, of a workgroup
   constexpr int RB = F8 ? D : 2 * D;              // bytes a row
   constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
   constexpr int KT = tile_keys(D, F8, GW);        // keys a tile
   constexpr int LOADS = KT / RPL, NS = KT / 32, NKK = D / 16, NDT = D / 32;
   constexpr int TB = KT * RB;                     // bytes of a tile; its scales: a dword a key
-  __shared__ __attribute__((aligned(1024))) uint8_t s_tiles[NW][2][2][TB];  // wave, K or V, buffer
-  __shared__ __attribute__((aligned(256))) uint32_t s_scales[NW][2][2][F8 ? 64 : 1];
+  __shared__ __attribute__((aligned(1024))) uint8_t s_tiles[WAVES][2][2][TB];  // wave, K or V, buffer
+  __shared__ __attribute__((aligned(256))) uint32_t s_scales[WAVES][2][2][F8 ? 64 : 1];
   const int lane = threadIdx.x & 63, l32 = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint8_t(*sK)[TB] = s_tiles[wave][0];
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : 1), GW > 1 ? 1 : 2) void paged_attn
     r = q / a.Hkv;
     h = q - r * a.Hkv;
   } else {
-    w = id;
+    w = id * kShareWaves + wave;
     team = w / a.Hkv;
     h = w - team * a.Hkv;
 
@@ -704,7 +705,7 @@ extern "C" int paged_attn_workspace(int R, int Hq, int Hkv, int D, int max_new, 
   g_err.clear();
   if (!bytes) return set_err(RA_EINVAL, "null pointer argument");
   if (int e = paged_check_heads(R, Hq, Hkv, D, max_new)) return e;
-  *bytes = paged_bytes(kMaxWorkers, paged_slots(Hq, Hkv, max_new), D);
+  *bytes = paged_bytes(max_workers(D), paged_slots(Hq, Hkv, max_new), D);
   return RA_OK;
 }
 
@@ -721,9 +722,9 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   const bool f8 = kv_type == RA_KV_E4M3;
   const int M = paged_slots(Hq, Hkv, max_new);
   const int rounds = (int)(((long long)max_new * (Hq / Hkv) + kSlots - 1) / kSlots);
-  const size_t need = paged_bytes(kMaxWorkers, M, D);
-  const int nw = std::max(workers(D, f8), Hkv);  // a team at least
-  static_assert(kMaxWorkers >= kMaxHeads);
+  const size_t need = paged_bytes(max_workers(D), M, D);
+  static_assert(workers(64, false) >= kMaxHeads && workers(128, false) >= kMaxHeads, "a team at least");
+  const int nw = workers(D, f8);
   if (workspace && workspace_bytes < need)
     return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   CallResources res(stream);
@@ -754,7 +755,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {
-      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : nw), dim3(64 * (gw ? gw : 1)), 0, stream, a);
+      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
       return hipGetLastError();
     });
   };

@@ -28,7 +28,6 @@ namespace {
 
 constexpr int kMaxNew = 32;      // new tokens a request
 constexpr int kSlots = 32;       // query slots a wave
-constexpr float kTau = 8.f;      // lazy-rescale threshold (log2 units)
 
 // Keys a tile, and the waves that share all tiles, four a workgroup: neighbouring key heads read pieces of
 // one token, so their waves stay close to one another in time and place (24 requests of 700 to 16001
@@ -164,6 +163,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
   constexpr int CPR = RB / 16, RPL = 64 / CPR;    // chunks a row; rows one 1 KB wave load fills
   constexpr int KT = tile_keys(D, F8, GW);        // keys a tile
   constexpr int LOADS = KT / RPL, NS = KT / 32, NKK = D / 16, NDT = D / 32;
+  constexpr float kTau = F8 ? 7.f : 8.f;          // lazy-rescale threshold (log2 units); 2^7 times a scale of 2^120 is finite
   constexpr int TB = KT * RB;                     // bytes of a tile; its scales: a dword a key
   __shared__ __attribute__((aligned(1024))) uint8_t s_tiles[WAVES][2][2][TB];  // wave, K or V, buffer
   __shared__ __attribute__((aligned(256))) uint32_t s_scales[WAVES][2][2][F8 ? 64 : 1];
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
       // keys that some row of the request does not see, or none does
       const bool diagonal = k0 + KT - 1 > q.first;
       const bool masked = diagonal || present != (KT == 64 ? ~0ull : (1ull << KT) - 1);
-      if (diagonal && q.n > 1) {
+      if (diagonal && q.first + 1 < q.keys) {  // (none such: every key is there for every row)
         // A value that is not finite, in a row that some slots see and some do not, would make NaN
         // of zero probabilities: its slots are noted, and it is overwritten by zero.
         bool odd = false;

@@ -247,3 +247,21 @@ def test_more_heads_than_waves_a_team(D, e4m3):
     check(s, *call(s, 3))
     s = make(61 + D, [90, 20], [1, 1], 900, 900, D, 16, e4m3, extra_cols=9000)
     check(s, *call(s, 1))
+
+
+@pytest.mark.parametrize("cols", [1, 3000])
+@pytest.mark.parametrize("max_new", [1, 2])
+def test_keys_of_rows_past_max_new_do_not_spread(max_new, cols):
+    """Requests of more rows than max_new: the rows that are computed see none of the later tokens,
+    whatever those hold; the others are left as they are."""
+    for e4m3 in (False, True):
+        s = make(70 + max_new, [60, 300], [5, 7], 8, 2, 128, 16, e4m3, extra_cols=cols)
+        for r, n in ((0, 5), (1, 7)):
+            for p in range(s["lens_np"][r] - n + max_new, s["lens_np"][r]):
+                i = s["table_np"][r, p // 16]
+                for t in ("k", "v"):
+                    if e4m3:
+                        s[t].view(torch.uint8)[i, p % 16] = 0x7f
+                    else:
+                        s[t][i, p % 16] = float("inf" if t == "v" else "nan")
+        check(s, *call(s, max_new), max_new)

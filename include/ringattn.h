@@ -374,7 +374,7 @@ int llama_stack_train_step(const void* x, const void* const* params, const void*
  *               the token's head is at most 448 in magnitude, 2^-126 at least (1 where all are
  *               zero), so that what a page stands for is exact in bf16 (above bf16's smallest
  *               numbers).  e4m3 has no infinity: infinite elements are stored as NaN.  Scales
- *               are 1 .. 254.
+ *               are 1 .. 254 of keys and 1 .. 247, the largest paged_append writes, of values.
  * page_size: a power of two, at most 1024; n_pages * page_size < 2^31; R <= 4096; heads <= 1024;
  * D in {64, 128}.  Device-side integers are not trusted: what lies out of range is left out, as
  * said at each call, and nothing out of bounds is read or written.
@@ -420,6 +420,7 @@ int paged_plan(const int* lens, const int* n_new, const int* free_pages, const i
  *   slots, positions in int32 [T] (paged_plan).  A row of a negative position is left out; one
  *             whose slot lies outside the cache has q rotated and nothing stored.  Two rows with
  *             one slot leave elements of either in it.
+ *   Outputs overlap no input, but q_out that is q.
  *   rotate    1: q and k are rotated by their positions (angles formed in double); 0: copied
  * T < 2^24.
  */
@@ -436,6 +437,8 @@ int paged_append(const void* q, const void* k, const void* v, void* q_out, void*
  *   cu_rows    in  int32 [R + 1] ascending, or NULL: row r is the one new token of request r
  *   max_new    the most new tokens of a request, <= 32; later rows of a longer one are not computed
  *   Row t of the n of request r sits at position lens[r] - n + t and sees keys up to its own.
+ *   Sums are float32 and relative to a maximum that may lag by up to 2^8: values of a magnitude
+ *   past 2^119 divided by the number of keys may come out infinite.
  *   Keys past max_pages pages, or in pages outside [0, n_pages), are masked.  A masked key counts
  *   for nothing, whatever its row holds; a row that sees no key has o = 0, lse = -inf.  Rows of
  *   no request are left as they are.
@@ -466,7 +469,7 @@ int paged_attn_decode(const void* q, const void* k_pages, const void* v_pages, c
  * scale is the smallest power of two (2^-126 at least) with which the group is at most 6 in
  * magnitude, codes are rounded to nearest, ties to the even code; a group with an infinity or NaN
  * has scale 255.
- * d_in % 32 == 0, d_in * d_out < 2^31, T <= 512.
+ * d_in % 32 == 0, d_in < 2^29, d_in * d_out < 2^31, T <= 512.  y may be residual; it overlaps no other input.
  */
 int mx4_pack(const void* w, void* w4, unsigned char* scales, int d_in, int d_out, hipStream_t stream);
 int mx4_linear(const void* x, const void* w4, const unsigned char* scales, const void* residual, void* y, int T,

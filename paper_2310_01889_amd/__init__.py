@@ -441,6 +441,8 @@ def _rows(t, name, T, H, D, dev):
         raise ValueError("the heads of a row of %s must be contiguous" % name)
     if t.dtype is not _BF16 or t.get_device() != dev:
         _arg(t[:1].contiguous(), name, _BF16, dev)  # says what is wrong
+    if T > 1 and row >> 31:
+        raise ValueError("the rows of %s lie %d elements apart: 2^31 - 1 at most" % (name, row))
     return t.data_ptr(), row if T > 1 else H * D
 
 

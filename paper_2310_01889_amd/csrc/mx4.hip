@@ -209,6 +209,7 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
 int check_mx(int K, int N) {
   if (K <= 0 || N <= 0) return set_err(RA_EINVAL, "sizes must be positive (d_in=%d d_out=%d)", K, N);
   if (K % 32) return set_err(RA_EUNSUPPORTED, "d_in=%d must be a multiple of 32", K);
+  if (K >= 1 << 29) return set_err(RA_EUNSUPPORTED, "d_in=%d exceeds 2^29-1", K);  // 2^24 workgroups of the packing
   if ((long long)K * N >= (1ll << 31)) return set_err(RA_EUNSUPPORTED, "d_in*d_out exceeds 2^31-1 elements");
   return RA_OK;
 }
@@ -237,6 +238,7 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
   if (int e = check_aligned({x, w4, residual, y}, {scales})) return e;
   if (T <= 0) return set_err(RA_EINVAL, "sizes must be positive (T=%d)", T);
   if (int e = check_mx(d_in, d_out)) return e;
+  if (x == y) return set_err(RA_EINVAL, "y must not be x");
   if (T > kMxMaxT) return set_err(RA_EUNSUPPORTED, "T=%d exceeds %d rows", T, kMxMaxT);
   MxArgs a{(const bf16*)x, (const uint8_t*)w4, scales, (const bf16*)residual, (bf16*)y, T, d_in, d_out,
            (d_in + 127) / 128};

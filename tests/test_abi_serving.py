@@ -104,3 +104,12 @@ def test_binding_checks_tensors_before_calling():
         ra._rows(torch.zeros(2, 1, 64, dtype=bf), "q", 3, 1, 64, 0)
     with pytest.raises(ValueError):
         ra._rows(torch.zeros(2, 64, 2, dtype=bf).transpose(1, 2), "q", 2, 2, 64, 0)
+
+
+def test_outputs_over_inputs_and_far_rows(lib):
+    assert lib.mx4_pack(P, P2, P3, 1 << 29, 1, NULL) == RA_EUNSUPPORTED
+    assert lib.mx4_linear(P, P2, P3, NULL, P, 1, 64, 64, NULL) == RA_EINVAL
+    assert b"y must not be x" in lib.ring_attn_last_error()
+    with pytest.raises(ValueError, match="apart"):
+        ra._rows(torch.empty((2, 1, 64), dtype=torch.bfloat16, device="meta").as_strided((2, 1, 64), (1 << 31, 64, 1)),
+                 "q", 2, 1, 64, -1)

@@ -407,7 +407,8 @@ def llama_stack_train_step(x, layer_params, dz, z, dx, layer_grads, n_heads, n_h
 
 
 # The calls of a decode step take a few microseconds on the GPU, so their checks are kept short: one
-# pass over a tensor in `_arg` (about half the host time of `_ptr`), the raw stream handle.
+# pass over a tensor in `_arg` (about half the host time of `_ptr`), the raw stream handle, the
+# library's function called by name.
 _BF16, _F32, _I32, _U8, _E4M3 = torch.bfloat16, torch.float32, torch.int32, torch.uint8, torch.float8_e4m3fn
 
 
@@ -424,12 +425,15 @@ def _arg(t, name, dtype, dev, shape=None):
 
 
 def _ints(t, name, n, dev):
-    """_arg of an int32 vector of n elements."""
-    if t is None:
-        return None
-    if t.dtype is _I32 and t.get_device() == dev and t.numel() == n and t.dim() == 1 and t.is_contiguous():
+    """_arg of n int32 elements."""
+    if t.dtype is _I32 and t.get_device() == dev and t.numel() == n and t.is_contiguous():
         return t.data_ptr()
     return _arg(t, name, _I32, dev, (n,))
+
+
+def _done(name, rc):
+    if rc:
+        raise RingAttnError(name, rc, load().ring_attn_last_error().decode())
 
 
 def _rows(t, name, T, H, D, dev):
@@ -471,13 +475,13 @@ def paged_plan(lens, n_new, free_pages, free_head, block_table, cu_rows, new_len
     """int32 tensors: lens, n_new, new_lens [R], free_pages [n_free], free_head [1] or None,
     block_table [R, max_pages], cu_rows [R + 1], slots, positions [T], counts [4]."""
     R, max_pages = block_table.shape
-    T, (dev, st) = slots.numel(), _current(stream)
-    _call("paged_plan", _ints(lens, "lens", R, dev), _ints(n_new, "n_new", R, dev),
-          _ints(free_pages, "free_pages", free_pages.numel(), dev), _ints(free_head, "free_head", 1, dev),
-          _arg(block_table, "block_table", _I32, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
-          _ints(new_lens, "new_lens", R, dev), _ints(slots, "slots", T, dev),
-          _ints(positions, "positions", T, dev), _ints(counts, "counts", 4, dev), R, page_size,
-          max_pages, n_pages, free_pages.numel(), T, st)
+    T, n_free, (dev, st) = slots.numel(), free_pages.numel(), _current(stream)
+    _done("paged_plan", (_LIB or load()).paged_plan(
+        _ints(lens, "lens", R, dev), _ints(n_new, "n_new", R, dev), _ints(free_pages, "free_pages", n_free, dev),
+        None if free_head is None else _ints(free_head, "free_head", 1, dev),
+        _arg(block_table, "block_table", _I32, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
+        _ints(new_lens, "new_lens", R, dev), _ints(slots, "slots", T, dev), _ints(positions, "positions", T, dev),
+        _ints(counts, "counts", 4, dev), R, page_size, max_pages, n_pages, n_free, T, st))
 
 
 def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=None, v_scales=None, rotate=True,
@@ -489,9 +493,10 @@ def paged_append(q, k, v, q_out, k_pages, v_pages, slots, positions, k_scales=No
     q_at, q_row = (None, 0) if q is None else _rows(q, "q", T, Hq, D, dev)
     k_at, k_row = _rows(k, "k", T, Hkv, D, dev)
     v_at, v_row = _rows(v, "v", T, Hkv, D, dev)
-    _call("paged_append", q_at, k_at, v_at, _arg(q_out, "q_out", _BF16, dev, (T, Hq, D)), kp, vp, ks, vs,
-          _ints(slots, "slots", T, dev), _ints(positions, "positions", T, dev), T, Hq, Hkv, D, q_row,
-          k_row, v_row, n_pages, page_size, kind, 1 if rotate else 0, st)
+    _done("paged_append", (_LIB or load()).paged_append(
+        q_at, k_at, v_at, _arg(q_out, "q_out", _BF16, dev, (T, Hq, D)), kp, vp, ks, vs, _ints(slots, "slots", T, dev),
+        _ints(positions, "positions", T, dev), T, Hq, Hkv, D, q_row, k_row, v_row, n_pages, page_size, kind,
+        1 if rotate else 0, st))
 
 
 def paged_attn_workspace(R, Hq, Hkv, D, max_new):
@@ -514,10 +519,11 @@ def paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, m
     ws, ws_bytes = None, 0
     if workspace is not None:
         ws, ws_bytes = _arg(workspace, "workspace", workspace.dtype, dev), workspace.numel() * workspace.element_size()
-    _call("paged_attn_decode", _arg(q, "q", _BF16, dev), kp, vp, ks, vs, _arg(block_table, "block_table", _I32, dev),
-          _ints(lens, "lens", R, dev), _ints(cu_rows, "cu_rows", R + 1, dev),
-          _arg(o, "o", _BF16, dev, (T, Hq, D)), _arg(lse, "lse", _F32, dev, (T, Hq)), ws, ws_bytes, T, R, Hq, Hkv, D,
-          n_pages, page_size, max_pages, max_new, kind, st)
+    _done("paged_attn_decode", (_LIB or load()).paged_attn_decode(
+        _arg(q, "q", _BF16, dev), kp, vp, ks, vs, _arg(block_table, "block_table", _I32, dev),
+        _ints(lens, "lens", R, dev), None if cu_rows is None else _ints(cu_rows, "cu_rows", R + 1, dev),
+        _arg(o, "o", _BF16, dev, (T, Hq, D)), _arg(lse, "lse", _F32, dev, (T, Hq)), ws, ws_bytes, T, R, Hq, Hkv, D,
+        n_pages, page_size, max_pages, max_new, kind, st))
 
 
 def mx4_pack(w, w4, scales, stream=None):
@@ -530,9 +536,10 @@ def mx4_pack(w, w4, scales, stream=None):
 def mx4_linear(x, w4, scales, residual, y, stream=None):
     (T, K), N, (dev, st) = x.shape, y.shape[1], _current(stream)
     nb, kb = -(-N // 16), -(-K // 128)
-    _call("mx4_linear", _arg(x, "x", _BF16, dev), _arg(w4, "w4", _U8, dev, (nb, kb, 64, 16)),
-          _arg(scales, "scales", _U8, dev, (nb, kb, 16, 4)), _arg(residual, "residual", _BF16, dev, (T, N)),
-          _arg(y, "y", _BF16, dev, (T, N)), T, K, N, st)
+    _done("mx4_linear", (_LIB or load()).mx4_linear(
+        _arg(x, "x", _BF16, dev), _arg(w4, "w4", _U8, dev, (nb, kb, 64, 16)),
+        _arg(scales, "scales", _U8, dev, (nb, kb, 16, 4)), _arg(residual, "residual", _BF16, dev, (T, N)),
+        _arg(y, "y", _BF16, dev, (T, N)), T, K, N, st))
 
 
 # ----------------------------------------------------------------------------------

@@ -181,19 +181,22 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
   const int id = xcd_swizzle(blockIdx.x, gridDim.x);
   int w = 0, team = 0, h, r;
   long long share = 0, u0 = 0, u1 = 1, r_at = 0;  // r_at: first unit of request r
+  Request q;                                      // request r
   if constexpr (GW > 0) {
-    const int q = id / a.rounds;
-    r = q / a.Hkv;
-    h = q - r * a.Hkv;
+    const int g = id / a.rounds;
+    r = g / a.Hkv;
+    h = g - r * a.Hkv;
+    q = request(a, r);
   } else {
     w = id * kShareWaves + wave;
     team = w / a.Hkv;
     h = w - team * a.Hkv;
 
     // ---- this team's share of the units ----
-    auto units = [&](int r) -> long long {  // of request r
+    auto units = [&](int r, Request& q) -> long long {  // of request r
+      q = Request{};
       if (r >= a.R) return 0;
-      const Request q = request(a, r);
+      q = request(a, r);
       const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
       return (long long)rounds * tiles;
     };
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     };
     const int per = (a.R + 63) / 64;  // requests a lane sums
     long long mine = 0;
-    for (int j = 0; j < per; ++j) mine += units(lane * per + j);
+    for (int j = 0; j < per; ++j) mine += units(lane * per + j, q);
     const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
     share = max(1ll, quotient(total + a.teams - 1, a.teams));
     u0 = share * team;
@@ -217,15 +220,21 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
     r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
     r_at = __shfl(upto - mine, r);
+    int at = r;
     if (per > 1) {
       r *= per;
-      const long long v = lane < per ? units(r + lane) : 0, s = scan(v);
-      const int k = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
-      r_at += __shfl(s - v, k);
-      r += k;
+      const long long v = lane < per ? units(r + lane, q) : 0, s = scan(v);
+      at = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(r_at + s > u0)) - 1;
+      r_at += __shfl(s - v, at);
+      r += at;
     }
     r = __builtin_amdgcn_readfirstlane(r);
     r_at = uniform(r_at);
+    at = __builtin_amdgcn_readfirstlane(at);  // the lane that has read request r
+    q.row0 = __builtin_amdgcn_readlane(q.row0, at);
+    q.n = __builtin_amdgcn_readlane(q.n, at);
+    q.keys = __builtin_amdgcn_readlane(q.keys, at);
+    q.first = __builtin_amdgcn_readlane(q.first, at);
   }
 
   // ---- constants of the tile loop ----
@@ -248,7 +257,6 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
 
   for (long long u = u0; u < u1;) {
     // ---- the group of unit u: request r, round of slots; its tiles [t0, t1) ----
-    Request q = request(a, r);
     int tiles, round, t0, t1;
     if constexpr (GW > 0) {
       tiles = max(1, (q.keys + KT - 1) / KT);
@@ -581,6 +589,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
 // added in order.  A workgroup is 8 waves: one slot (groups are few, their parts many) or eight
 // (see the choice at the launch).  The weights 2^(m - M) are formed by the lanes, 64 parts at a time.
 constexpr int kJoinWaves = 8;
+constexpr int kEarly = 8;  // parts whose loads do not wait for the weights
 
 template <int D, int WPS>
 __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const PagedArgs a) {
@@ -588,38 +597,51 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const Paged
   __shared__ float s_sum[kJoinWaves][D + 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.Hq / a.Hkv;
   const int slot = blockIdx.y * (kJoinWaves / WPS) + wave / WPS, w = wave % WPS;
+  const Split sp = a.split[blockIdx.x];
   if (a.by_group) {  // an entry is there if its request has such a round
     const int g = blockIdx.x / a.rounds, round = blockIdx.x - g * a.rounds;
     if (request(a, g / a.Hkv).n * G <= round * kSlots) return;
   }
-  const Split sp = a.split[blockIdx.x];
   if (sp.parts == 0 || (int)blockIdx.y * (kJoinWaves / WPS) >= sp.slots) return;
   const bool on = slot < sp.slots;  // (the waves of a workgroup meet at its barriers)
   auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i * a.Hkv)) * a.M + slot; };
   // the largest maximum of this wave's parts, then their sums relative to it
   const int mine = on ? (sp.parts - w + WPS - 1) / WPS : 0;  // parts w, w + WPS, ...
-  float m = -INFINITY;
-  for (int i = lane; i < mine; i += 64) m = fmaxf(m, a.part_ml[2 * part(w + i * WPS)]);
+  float acc[E], x[kEarly][E];
+#pragma unroll
+  for (int i = 0; i < kEarly; ++i)  // the first parts are on their way while their weights are formed
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      x[i][e] = i < mine ? a.part_acc[part(w + i * WPS) * D + lane + 64 * e] : 0.f;
+  const f32x2 none = {-INFINITY, 0.f};
+  const f32x2 ml0 = lane < mine ? *(const f32x2*)(a.part_ml + 2 * part(w + lane * WPS)) : none;
+  float m = ml0[0];
+  for (int i = lane + 64; i < mine; i += 64) m = fmaxf(m, a.part_ml[2 * part(w + i * WPS)]);
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
   const float m_eff = m == -INFINITY ? 0.f : m;
-  float l = 0.f, acc[E];
+  float l = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.f;
   for (int i0 = 0; i0 < mine; i0 += 64) {
-    float wt = 0.f;
-    if (i0 + lane < mine) {
-      const f32x2 ml = *(const f32x2*)(a.part_ml + 2 * part(w + (i0 + lane) * WPS));
-      wt = ml[1] == 0.f ? 0.f : exp2f(ml[0] - m_eff);
-      l = fmaf(ml[1], wt, l);
-    }
+    const f32x2 ml = i0 == 0 ? ml0 : i0 + lane < mine ? *(const f32x2*)(a.part_ml + 2 * part(w + (i0 + lane) * WPS)) : none;
+    const float wt = ml[1] == 0.f ? 0.f : exp2f(ml[0] - m_eff);
+    l = fmaf(ml[1], wt, l);
     const int n = min(64, mine - i0);
-#pragma unroll 8
-    for (int i = 0; i < n; ++i) {
-      const float* x = a.part_acc + part(w + (i0 + i) * WPS) * D;
-      const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), i));
+    auto weight = [&](int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wt), i)); };
+    if (i0 == 0) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(x[lane + 64 * e], wi, acc[e]);
+      for (int i = 0; i < kEarly; ++i)
+        if (i < n)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = fmaf(x[i][e], weight(i), acc[e]);
+    }
+#pragma unroll 8
+    for (int i = i0 == 0 ? kEarly : 0; i < n; ++i) {
+      const float* y = a.part_acc + part(w + (i0 + i) * WPS) * D;
+      const float wi = weight(i);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = fmaf(y[lane + 64 * e], wi, acc[e]);
     }
   }
 #pragma unroll

@@ -762,18 +762,19 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
               groups <= nw, nw / Hkv, 1.f / sqrtf((float)D)};
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
-  // where the groups fill the chip or the tiles (8 KB of keys, 64 keys at most) are few, four waves
-  // where the groups are at most one a compute unit; else shares of all tiles and a second launch.
-  // us with one wave, four, shares; bf16, requests of a quarter of the keys to all of them:
-  //   1024 groups of 128 dims: 120 keys 11.2, 19.0, 19.1; 500 36.8, 45.6, 42.3; 1000 71.6, 74.6,
-  //   73.1; 2000 138.6, 134.9, 130.0.  256 groups of 64 dims: 120 keys 7.5, 7.4, 10.3; 500 13.9, 8.8,
-  //   16.1; 1000 24.6, 13.3, 19.1.  16 groups of 128: 120 keys 7.2, 7.7, 10.2; 500 17.8, 9.3, 11.9;
-  //   1000 32.4, 14.6, 12.2.
+  // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
+  // they do not and the tiles are no more than a launch and a half's time; else shares of all tiles and
+  // a second launch.  us with one wave, four, shares; one token a request, of a quarter of the keys to all:
+  //   1024 groups of 128 dims in bf16: 120 keys 11.3, 19.0, 21.3; 500 31.9, 39.1, 38.0; 1000 68.0, 75.6,
+  //   64.8.  512 groups: 120 8.3, 9.9, 15.7; 500 25.8, 22.0, 24.9; 1000 45.1, 34.0, 35.8; 1500 64.4, 46.8,
+  //   44.7.  128 groups: 250 11.6, 7.9, 11.4; 1000 40.3, 17.1, 19.6; 1500 57.6, 23.5, 22.4; in 8 bits 1000
+  //   38.2, 15.1, 19.3; 2000 76.3, 25.2, 23.9.  16 groups: 120 7.9, 7.9, 11.2; 500 20.4, 9.9, 11.6; 1000
+  //   37.2, 15.9, 11.8.  256 groups of 64 dims in bf16: 500 14.3, 8.1, 14.1; 2000 52.3, 23.7, 24.3.
   const long long keys = (long long)max_pages * page_size, kt = f8 || D == 64 ? 64 : 32, tiles = (keys + kt - 1) / kt;
   int gw = 0;
-  if (groups >= 1024) gw = keys <= 1024 ? 1 : 0;
-  else if (groups > 256) gw = tiles <= 8 ? 1 : 0;
-  else gw = tiles <= 2 ? 1 : tiles <= 16 ? 4 : 0;
+  if (groups >= 1024) gw = keys <= 768 ? 1 : 0;
+  else if (groups > 256) gw = tiles <= 8 ? 1 : tiles <= 32 ? 4 : 0;
+  else gw = tiles <= 2 ? 1 : tiles <= (groups > 64 ? 32 : 16) ? 4 : 0;
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {

@@ -265,3 +265,13 @@ def test_keys_of_rows_past_max_new_do_not_spread(max_new, cols):
                     else:
                         s[t][i, p % 16] = float("inf" if t == "v" else "nan")
         check(s, *call(s, max_new), max_new)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("D,keys", [(128, 500), (64, 900), (128, 1100)])
+def test_many_requests_of_middling_length(D, keys, e4m3):
+    """512 groups of requests and key heads: four waves a group up to 32 tiles, shares beyond."""
+    lens = [keys - (keys * i) // 70 for i in range(64)]
+    news = [1 + i % 3 for i in range(64)]
+    s = make(80 + D, lens, news, 16, 8, D, 16, e4m3)
+    check(s, *call(s, 3))

@@ -248,14 +248,16 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
   //   32 x 4096 x 4096   7.5  5.2  6.8  6.7  -     -        20 x 4096 x 2048   4.6  4.9  6.6  6.2  -  -
   //   48 x 11008 x 4096  20.6 18.6 15.6 15.6 20.6  -        48 x 4096 x 11008  -  15.8 17.2 16.9 16.5 13.2
   //   96 x 4096 x 11008  -    25.9 25.3 24.5 20.6  21.0
-  // 4x4 for 64 x 4096 x 11008: 16.8 us, 2x4 17.9.  NB = 4 with several tiles, one stage: eight waves where
-  // every workgroup has a compute unit of its own (24 x 4096 x 11008 10.9 us, four waves 15.4), else four,
-  // two workgroups a unit (300 x 4096 x 4096 18.3, eight waves 20.6).  1x1 and up to eight rows: 16 waves
-  // in the first case (1 x 11008 x 4096 6.6 us, eight waves 8.1).
+  // 4x4 for 64 x 4096 x 11008: 16.8 us, 2x4 17.9.  Three blocks where two need two rounds of the chip and
+  // four leave units idle: 7 x 4096 x 11008 7.2 us, 1x4 7.9; 24 x 4096 x 11008 10.1, 2x4 10.8; 48 rows 12.2, 3x4
+  // 13.3.  Several tiles of three and more blocks, one stage: eight waves where every workgroup has a compute
+  // unit of its own (24 x 4096 x 11008 10.9 us, four waves 15.4), else four, two workgroups a unit (300 x
+  // 4096 x 4096 18.3, eight waves 20.6).  1x1 and up to eight rows: 16 waves (1 x 11008 x 4096 6.6 us, eight
+  // waves 8.1).
   const int tiles = (T + 15) / 16, blocks = (d_out + 15) / 16;
   const int xl = T <= 4 ? 1 : T <= 8 ? 2 : 4;
   auto groups = [&](int nt, int nb) { return (long long)((blocks + nb - 1) / nb) * ((tiles + nt - 1) / nt); };
-  static constexpr int kPairs[][2] = {{4, 4}, {3, 4}, {2, 4}, {2, 2}, {1, 4}, {1, 2}, {1, 1}};
+  static constexpr int kPairs[][2] = {{4, 4}, {3, 4}, {3, 3}, {2, 4}, {2, 3}, {2, 2}, {1, 4}, {1, 3}, {1, 2}, {1, 1}};
   int nt = 1, nb = 1;
   long long least = LLONG_MAX;
   for (const auto& p : kPairs) {
@@ -268,20 +270,23 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
     hipLaunchKernelGGL(kernel, dim3((blocks + nb - 1) / nb, (tiles + nt - 1) / nt), dim3(64 * wv), 0, stream, a);
   };
   auto one_tile = [&](auto* four, auto* eight, auto* sixteen) { run(xl == 1 ? four : xl == 2 ? eight : sixteen, 8); };
-  if (nt == 1 && nb == 1 && wide && xl < 4)
-    run(xl == 1 ? mx4_linear_kernel<1, 1, 16, true, 1> : mx4_linear_kernel<1, 1, 16, true, 2>, 16);
+  if (nt == 1 && nb == 1 && xl == 4) run(mx4_linear_kernel<1, 1, 8, true>, 8);
   else if (nt == 1 && nb == 1)
-    one_tile(mx4_linear_kernel<1, 1, 8, true, 1>, mx4_linear_kernel<1, 1, 8, true, 2>, mx4_linear_kernel<1, 1, 8, true>);
+    run(xl == 1 ? mx4_linear_kernel<1, 1, 16, true, 1> : mx4_linear_kernel<1, 1, 16, true, 2>, 16);
   else if (nt == 1 && nb == 2)
     one_tile(mx4_linear_kernel<1, 2, 8, true, 1>, mx4_linear_kernel<1, 2, 8, true, 2>, mx4_linear_kernel<1, 2, 8, true>);
+  else if (nt == 1 && nb == 3)
+    one_tile(mx4_linear_kernel<1, 3, 8, true, 1>, mx4_linear_kernel<1, 3, 8, true, 2>, mx4_linear_kernel<1, 3, 8, true>);
   else if (nt == 1)
     one_tile(mx4_linear_kernel<1, 4, 8, true, 1>, mx4_linear_kernel<1, 4, 8, true, 2>, mx4_linear_kernel<1, 4, 8, true>);
   else if (nt == 2 && nb == 2) run(mx4_linear_kernel<2, 2, 7, true>, 7);
-  else if (nt == 2 && wide) run(mx4_linear_kernel<2, 4, 8, false>, 8);
-  else if (nt == 2) run(mx4_linear_kernel<2, 4, 4, false>, 4);
-  else if (nt == 3 && wide) run(mx4_linear_kernel<3, 4, 8, false>, 8);
-  else if (nt == 3) run(mx4_linear_kernel<3, 4, 4, false>, 4);
-  else run(mx4_linear_kernel<4, 4, 8, false>, 8);
+  else if (nt == 4) run(mx4_linear_kernel<4, 4, 8, false>, 8);
+  else if (wide)
+    run(nt == 2 ? (nb == 3 ? mx4_linear_kernel<2, 3, 8, false> : mx4_linear_kernel<2, 4, 8, false>)
+                : (nb == 3 ? mx4_linear_kernel<3, 3, 8, false> : mx4_linear_kernel<3, 4, 8, false>), 8);
+  else
+    run(nt == 2 ? (nb == 3 ? mx4_linear_kernel<2, 3, 4, false> : mx4_linear_kernel<2, 4, 4, false>)
+                : (nb == 3 ? mx4_linear_kernel<3, 3, 4, false> : mx4_linear_kernel<3, 4, 4, false>), 4);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

@@ -66,7 +66,8 @@ def test_linear(T, K, N, residual):
 @pytest.mark.parametrize("T,K,N", [
     (1, 2208, 9005), (1, 2208, 4100), (2, 1184, 14000), (5, 1184, 20000), (7, 2208, 5003), (8, 1184, 11000),
     (9, 4256, 1000), (12, 1184, 20000), (16, 2208, 8190), (11, 2208, 9005), (20, 2208, 6001), (20, 416, 20000),
-    (31, 1184, 11000), (70, 416, 9005), (40, 1184, 12001), (90, 1056, 11000), (60, 1184, 9005), (200, 416, 8190)])
+    (31, 1184, 11000), (70, 416, 9005), (40, 1184, 12001), (90, 1056, 11000), (60, 1184, 9005), (200, 416, 8190),
+    (6, 1184, 13001), (15, 1184, 14000), (23, 1184, 7000), (18, 1184, 13000), (66, 416, 13003), (45, 416, 15999)])
 def test_linear_in_every_shape_of_workgroup(T, K, N):
     """Rows and outputs that take each number of row tiles and output blocks a workgroup, with a
     ragged end each; more inputs than the waves of one take at a time."""

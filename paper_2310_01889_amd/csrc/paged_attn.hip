@@ -763,18 +763,21 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
-  // they do not and the tiles are no more than a launch and a half's time; else shares of all tiles and
-  // a second launch.  us with one wave, four, shares; one token a request, of a quarter of the keys to all:
+  // they do not and their turns take no longer than a second launch; else shares of all tiles and that
+  // second launch.  us with one wave, four, shares; one token a request, of a quarter of the keys to all:
   //   1024 groups of 128 dims in bf16: 120 keys 11.3, 19.0, 21.3; 500 31.9, 39.1, 38.0; 1000 68.0, 75.6,
   //   64.8.  512 groups: 120 8.3, 9.9, 15.7; 500 25.8, 22.0, 24.9; 1000 45.1, 34.0, 35.8; 1500 64.4, 46.8,
   //   44.7.  128 groups: 250 11.6, 7.9, 11.4; 1000 40.3, 17.1, 19.6; 1500 57.6, 23.5, 22.4; in 8 bits 1000
   //   38.2, 15.1, 19.3; 2000 76.3, 25.2, 23.9.  16 groups: 120 7.9, 7.9, 11.2; 500 20.4, 9.9, 11.6; 1000
   //   37.2, 15.9, 11.8.  256 groups of 64 dims in bf16: 500 14.3, 8.1, 14.1; 2000 52.3, 23.7, 24.3.
+  // Four waves, shares; of a third of the keys to all:  58 groups, one token 1000 16.3, 17.3; 1500 23.0, 17.3;
+  //   four tokens of 8 heads 1000 19.2, 27.3; 1500 25.4, 26.7.  32 groups 600 11.3, 12.4; 1000 15.8, 12.0.
+  //   320 groups, four tokens of 4 heads 600 25.7, 26.3; 1000 32.8, 30.2; in 8 bits 600 22.9, 24.7.
   const long long keys = (long long)max_pages * page_size, kt = f8 || D == 64 ? 64 : 32, tiles = (keys + kt - 1) / kt;
   int gw = 0;
   if (groups >= 1024) gw = keys <= 768 ? 1 : 0;
-  else if (groups > 256) gw = tiles <= 8 ? 1 : tiles <= 32 ? 4 : 0;
-  else gw = tiles <= 2 ? 1 : tiles <= (groups > 64 ? 32 : 16) ? 4 : 0;
+  else if (groups > 256) gw = tiles <= 8 ? 1 : keys <= 768 ? 4 : 0;
+  else gw = tiles <= 2 ? 1 : keys <= (groups > 48 ? 1152 : 640) ? 4 : 0;
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {

@@ -270,7 +270,8 @@ def test_keys_of_rows_past_max_new_do_not_spread(max_new, cols):
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("D,keys", [(128, 500), (64, 900), (128, 1100)])
 def test_many_requests_of_middling_length(D, keys, e4m3):
-    """512 groups of requests and key heads: four waves a group up to 32 tiles, shares beyond."""
+    """512 groups of requests and key heads: four waves a group for tables of up to 768 keys, shares
+    beyond."""
     lens = [keys - (keys * i) // 70 for i in range(64)]
     news = [1 + i % 3 for i in range(64)]
     s = make(80 + D, lens, news, 16, 8, D, 16, e4m3)

@@ -434,10 +434,10 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
           thr = (m_new == -INFINITY) ? -INFINITY : kTau;
         }
         // Probabilities; the denominator sums them as they are, the products take them as the sum of
-        // two bf16 numbers, the one next below and the rounding of what that leaves (both above zero
-        // where the probability is: an infinite value has an infinite sum).  Rounded to one number
-        // they put o up to 1.5 times as far from float64 as its own storage in bf16 does (262144
-        // keys: 2.4e-3 against 1.6e-3); the second product hides behind the loads.
+        // three bf16 numbers, which is exact: the one next below, the one next below what that leaves,
+        // and the rest, 8 bits at most.  (With two they are off by up to 2^-16, which outputs that
+        // nearly cancel show.)  All three are above zero where the probability is, 2^-126 at least:
+        // an infinite value has an infinite sum (8 bits hold none).
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
 #pragma unroll
@@ -452,18 +452,28 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
               s[8 * g + e] = __builtin_ldexpf(s[8 * g + e], (int)(e < 4 ? lo[e & 3] : up[e & 3]) - 127);
           }
         }
-        bf16x8 pb[2], pl[2];
+        bf16x8 pb[3][2];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          u32x4 pw, pr;
+          u32x4 w[3];
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float p0 = s[8 * g + 2 * j], p1 = s[8 * g + 2 * j + 1];
-            pw[j] = bf16x2_below(p0, p1);
-            pr[j] = pack_bf16x2(p0 - __uint_as_float(pw[j] << 16), p1 - __uint_as_float(pw[j] & 0xffff0000u));
+            float p0 = s[8 * g + 2 * j], p1 = s[8 * g + 2 * j + 1];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              w[e][j] = bf16x2_below(p0, p1);
+              p0 -= __uint_as_float(w[e][j] << 16);
+              p1 -= __uint_as_float(w[e][j] & 0xffff0000u);
+            }
+            w[2][j] = pack_bf16x2(p0, p1);
+            if constexpr (!F8) {
+              const uint32_t least = min_u16x2(w[0][j], 0x800080u);
+              w[1][j] = max_u16x2(w[1][j], least);
+              w[2][j] = max_u16x2(w[2][j], least);
+            }
           }
-          pb[g] = __builtin_bit_cast(bf16x8, pw);
-          pl[g] = __builtin_bit_cast(bf16x8, pr);
+#pragma unroll
+          for (int e = 0; e < 3; ++e) pb[e][g] = __builtin_bit_cast(bf16x8, w[e]);
         }
         const uint8_t* vs = vt + 32 * sub * RB;
         auto values = [&](int g, int dt) __attribute__((always_inline)) {  // 16 keys x 32 dims of V^T
@@ -484,8 +494,8 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
 #pragma unroll
           for (int dt = 0; dt < NDT; ++dt) {
             const bf16x8 vv = values(g, dt);
-            oacc[dt] = mfma32(vv, pb[g], oacc[dt]);
-            oacc[dt] = mfma32(vv, pl[g], oacc[dt]);
+#pragma unroll
+            for (int e = 0; e < 3; ++e) oacc[dt] = mfma32(vv, pb[e][g], oacc[dt]);
           }
       }
     }

@@ -113,6 +113,15 @@ __device__ __forceinline__ uint32_t bf16x2_below(float a, float b) {
   return __builtin_amdgcn_perm(y, x, 0x07060302u);
 }
 
+// Smaller and larger of the halves of two dwords, as whole numbers.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t min_u16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 // Map a linear workgroup id so that each XCD (workgroups are dispatched round-robin
 // over the 8 XCDs) receives a contiguous range of logical tiles: tiles that share
 // key/value data then share one L2.

@@ -759,18 +759,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   const int nw = workers(D, f8);
   if (workspace && workspace_bytes < need)
     return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
-  CallResources res(stream);
-  if (!workspace) {
-    if ((rc = res.alloc(need))) return rc;
-    workspace = res.ws;
-  }
   const long long groups = (long long)R * Hkv * rounds;
-  float* acc = (float*)workspace;
-  float* ml = acc + (size_t)nw * 2 * M * D;
-  PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, acc, ml,
-              (Split*)(ml + (size_t)nw * 2 * M * 2), T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds,
-              groups <= nw, nw / Hkv, 1.f / sqrtf((float)D)};
-  while ((1 << a.page_shift) < page_size) ++a.page_shift;
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
   // they do not and their turns take no longer than a second launch; else shares of all tiles and that
@@ -788,6 +777,20 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   if (groups >= 1024) gw = keys <= 768 ? 1 : 0;
   else if (groups > 256) gw = tiles <= 8 ? 1 : keys <= 768 ? 4 : 0;
   else gw = tiles <= 2 ? 1 : keys <= (groups > 48 ? 1152 : 640) ? 4 : 0;
+  CallResources res(stream);
+  if (!workspace && gw == 0) {  // (one launch keeps nothing in it)
+    if ((rc = res.alloc(paged_bytes(nw, M, D)))) return rc;
+    workspace = res.ws;
+  }
+  PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, nullptr,
+              nullptr, nullptr, T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds, groups <= nw, nw / Hkv,
+              1.f / sqrtf((float)D)};
+  if (gw == 0) {
+    a.part_acc = (float*)workspace;
+    a.part_ml = a.part_acc + (size_t)nw * 2 * M * D;
+    a.split = (Split*)(a.part_ml + (size_t)nw * 2 * M * 2);
+  }
+  while ((1 << a.page_shift) < page_size) ++a.page_shift;
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {

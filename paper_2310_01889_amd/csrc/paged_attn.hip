@@ -13,6 +13,7 @@
 // same time.  The lengths are on the device: each wave finds its team's share from their prefix
 // sums itself.  A wave whose share holds a whole (request, round) writes its result; the others
 // leave partial softmax states that a second launch joins.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -595,24 +596,19 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
 }
 
 // Joins the parts of the groups that several waves share.  WPS waves take one query slot of one
-// entry: each sums every WPS-th part, its loads independent of one another, and their sums are
-// added in order.  A workgroup is 8 waves: one slot (groups are few, their parts many) or eight
-// (see the choice at the launch).  The weights 2^(m - M) are formed by the lanes, 64 parts at a time.
+// entry: each sums every WPS-th part, kBatch loads of them in flight together, and their sums are added
+// in order.  A workgroup is 8 waves: one slot or eight (see the choice at the launch).  The weights
+// 2^(m - M) are formed by the lanes, 64 parts at a time.
 constexpr int kJoinWaves = 8;
-constexpr int kEarly = 8;  // parts whose loads do not wait for the weights
+constexpr int kEarly = 8;   // parts whose loads do not wait for the weights
+constexpr int kBatch = 16;  // (8 slots of 940 parts, a wave each: 257 us with one load after the other, 90 so)
+constexpr int kLongParts = 64;  // (see the launch)
 
 template <int D, int WPS>
-__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const PagedArgs a) {
+__device__ __forceinline__ void join_slot(const PagedArgs& a, const Split& sp, int slot, float (*s_sum)[D + 2]) {
   constexpr int E = D / 64;
-  __shared__ float s_sum[kJoinWaves][D + 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), G = a.Hq / a.Hkv;
-  const int slot = blockIdx.y * (kJoinWaves / WPS) + wave / WPS, w = wave % WPS;
-  const Split sp = a.split[blockIdx.x];
-  if (a.by_group) {  // an entry is there if its request has such a round
-    const int g = blockIdx.x / a.rounds, round = blockIdx.x - g * a.rounds;
-    if (request(a, g / a.Hkv).n * G <= round * kSlots) return;
-  }
-  if (sp.parts == 0 || (int)blockIdx.y * (kJoinWaves / WPS) >= sp.slots) return;
+  const int w = wave % WPS;
   const bool on = slot < sp.slots;  // (the waves of a workgroup meet at its barriers)
   auto part = [&](int i) { return ((long long)(i == 0 ? sp.first : (sp.first & ~1) + 2 * i * a.Hkv)) * a.M + slot; };
   // the largest maximum of this wave's parts, then their sums relative to it
@@ -646,12 +642,20 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const Paged
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[e] = fmaf(x[i][e], weight(i), acc[e]);
     }
-#pragma unroll 8
-    for (int i = i0 == 0 ? kEarly : 0; i < n; ++i) {
-      const float* y = a.part_acc + part(w + (i0 + i) * WPS) * D;
-      const float wi = weight(i);
+#pragma unroll 1
+    for (int i = i0 == 0 ? kEarly : 0; i < n; i += kBatch) {
+      float y[kBatch][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(y[lane + 64 * e], wi, acc[e]);
+      for (int j = 0; j < kBatch; ++j) {
+        const float* at = a.part_acc + part(w + (i0 + min(i + j, n - 1)) * WPS) * D + lane;
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[j][e] = at[64 * e];
+      }
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (i + j < n)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] = fmaf(y[j][e], weight(i + j), acc[e]);
     }
   }
 #pragma unroll
@@ -688,6 +692,27 @@ __global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const Paged
 #pragma unroll
   for (int e = 0; e < E; ++e) a.o[qrow * D + lane + 64 * e] = (bf16)(acc[e] * inv);
   if (lane == 0) a.lse[qrow] = l == 0.f ? -INFINITY : top * kLn2 + logf(l);
+}
+
+// FEW: eight waves a slot.  Else a wave a slot, but for entries of more than `longer` parts.
+template <int D, bool FEW>
+__global__ __launch_bounds__(64 * kJoinWaves) void paged_join_kernel(const PagedArgs a, int longer) {
+  __shared__ float s_sum[kJoinWaves][D + 2];
+  const Split sp = a.split[blockIdx.x];
+  if (a.by_group) {  // an entry is there if its request has such a round
+    const int g = blockIdx.x / a.rounds, round = blockIdx.x - g * a.rounds;
+    if (request(a, g / a.Hkv).n * (a.Hq / a.Hkv) <= round * kSlots) return;
+  }
+  if (sp.parts == 0) return;
+  const int y = blockIdx.y;
+  if (FEW || sp.parts > longer) {
+    for (int slot = y; slot < sp.slots; slot += gridDim.y) {
+      if (slot != y) __syncthreads();  // the last slot's sums have been read
+      join_slot<D, kJoinWaves>(a, sp, slot, s_sum);
+    }
+  } else if (y * kJoinWaves < sp.slots) {
+    join_slot<D, 1>(a, sp, y * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), s_sum);
+  }
 }
 
 }  // namespace
@@ -807,12 +832,18 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
                         : launch(paged_attn_kernel<64, false, 0>, paged_attn_kernel<64, false, 1>,
                                  paged_attn_kernel<64, false, 4>)));
   if (gw) return RA_OK;
-  // few groups: many parts each, a workgroup a slot; many: few parts, a wave a slot
-  const bool few = groups <= 64;
-  const dim3 grid(a.by_group ? (unsigned)groups : nw, few ? M : (M + kJoinWaves - 1) / kJoinWaves);
-  auto* join = D == 128 ? (few ? paged_join_kernel<128, kJoinWaves> : paged_join_kernel<128, 1>)
-                        : (few ? paged_join_kernel<64, kJoinWaves> : paged_join_kernel<64, 1>);
-  hipLaunchKernelGGL(join, grid, dim3(64 * kJoinWaves), 0, stream, a);
+  // Few groups: many parts each, a workgroup a slot.  Many: few parts, a wave a slot; but of requests of
+  // very different lengths one may still have a part of every team.  Where the teams are many, the slots of
+  // entries of more than kLongParts parts are dealt to workgroups of their own, 2048 in all at most, for
+  // most find nothing to do (400 entries of 32 slots: 124 us with a workgroup a slot, 96 so); with up to
+  // 256 parts a wave a slot will do.  One request of 60000 tokens alone, 8 heads over one key head: 27 us;
+  // among 69 of five tokens 104 with a wave a slot, 30 so; among 900 84 and 62.
+  const bool few = groups <= 64, long_lists = !few && a.teams > 256;
+  const int entries = a.by_group ? (int)groups : nw, least = (M + kJoinWaves - 1) / kJoinWaves;
+  const dim3 grid(entries, few ? M : long_lists ? std::min(M, std::max(least, 2048 / entries)) : least);
+  auto* join = D == 128 ? (few ? paged_join_kernel<128, true> : paged_join_kernel<128, false>)
+                        : (few ? paged_join_kernel<64, true> : paged_join_kernel<64, false>);
+  hipLaunchKernelGGL(join, grid, dim3(64 * kJoinWaves), 0, stream, a, long_lists ? kLongParts : INT_MAX);
   RA_HIP(hipGetLastError());
   return RA_OK;
 }

@@ -180,26 +180,21 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
   };
   // neighbours of one XCD: what the heads of a request read side by side (ids, scales) shares an L2
   const int id = xcd_swizzle(blockIdx.x, gridDim.x);
-  int w = 0, team = 0, h, r;
+  int w = 0, team = 0, h, r, round = 0;
   long long share = 0, u0 = 0, u1 = 1, r_at = 0;  // r_at: first unit of request r
   Request q;                                      // request r
-  if constexpr (GW > 0) {
-    const int g = id / a.rounds;
-    r = g / a.Hkv;
-    h = g - r * a.Hkv;
+  if (GW > 0 && a.rounds == 1) {  // a workgroup a (request, key head), of whatever requests have rows
+    r = id / a.Hkv;
+    h = id - r * a.Hkv;
     q = request(a, r);
   } else {
-    w = id * kShareWaves + wave;
-    team = w / a.Hkv;
-    h = w - team * a.Hkv;
-
-    // ---- this team's share of the units ----
+    // ---- this team's share of the units, or the one (request, round) of a workgroup's heads ----
     auto units = [&](int r, Request& q) -> long long {  // of request r
       q = Request{};
       if (r >= a.R) return 0;
       q = request(a, r);
       const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
-      return (long long)rounds * tiles;
+      return GW > 0 ? rounds : (long long)rounds * tiles;
     };
     auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
 #pragma unroll
@@ -213,11 +208,21 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     long long mine = 0;
     for (int j = 0; j < per; ++j) mine += units(lane * per + j, q);
     const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
-    share = max(1ll, quotient(total + a.teams - 1, a.teams));
-    u0 = share * team;
-    u1 = min(total, u0 + share);
-    if (!a.by_group && lane == 0) a.split[w].parts = 0;
-    if (team >= a.teams || u0 >= u1) return;
+    if constexpr (GW > 0) {
+      u0 = id / a.Hkv;
+      h = id - (int)u0 * a.Hkv;
+      u1 = u0 + 1;
+      if (u0 >= total) return;
+    } else {
+      w = id * kShareWaves + wave;
+      team = w / a.Hkv;
+      h = w - team * a.Hkv;
+      share = max(1ll, quotient(total + a.teams - 1, a.teams));
+      u0 = share * team;
+      u1 = min(total, u0 + share);
+      if (!a.by_group && lane == 0) a.split[w].parts = 0;
+      if (team >= a.teams || u0 >= u1) return;
+    }
     // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
     r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
     r_at = __shfl(upto - mine, r);
@@ -236,6 +241,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     q.n = __builtin_amdgcn_readlane(q.n, at);
     q.keys = __builtin_amdgcn_readlane(q.keys, at);
     q.first = __builtin_amdgcn_readlane(q.first, at);
+    if constexpr (GW > 0) round = (int)(u0 - r_at);
   }
 
   // ---- constants of the tile loop ----
@@ -258,10 +264,9 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
 
   for (long long u = u0; u < u1;) {
     // ---- the group of unit u: request r, round of slots; its tiles [t0, t1) ----
-    int tiles, round, t0, t1;
+    int tiles, t0, t1;
     if constexpr (GW > 0) {
       tiles = max(1, (q.keys + KT - 1) / KT);
-      round = id % a.rounds;
       if (round * kSlots >= q.n * G) return;
       t0 = wave;
       t1 = tiles;
@@ -785,6 +790,11 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   if (workspace && workspace_bytes < need)
     return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   const long long groups = (long long)R * Hkv * rounds;
+  // Groups that the rows can make, whatever max_new allows (by rounds of slots): a round a request that has a row, and as 32 / G
+  // tokens are a round at most (a token G / 32, where G is larger), one for so many of the other rows.
+  const int some = std::min(R, T), G = Hq / Hkv;
+  const long long real = std::min(groups, Hkv * (long long)((G + kSlots - 1) / kSlots) *
+                                              (some + (T - some) / std::max(1, kSlots / G)));
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
   // they do not and their turns take no longer than a second launch; else shares of all tiles and that
@@ -799,9 +809,9 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   //   320 groups, four tokens of 4 heads 600 25.7, 26.3; 1000 32.8, 30.2; in 8 bits 600 22.9, 24.7.
   const long long keys = (long long)max_pages * page_size, kt = f8 || D == 64 ? 64 : 32, tiles = (keys + kt - 1) / kt;
   int gw = 0;
-  if (groups >= 1024) gw = keys <= 768 ? 1 : 0;
-  else if (groups > 256) gw = tiles <= 8 ? 1 : keys <= 768 ? 4 : 0;
-  else gw = tiles <= 2 ? 1 : keys <= (groups > 48 ? 1152 : 640) ? 4 : 0;
+  if (real >= 1024) gw = keys <= 768 ? 1 : 0;
+  else if (real > 256) gw = tiles <= 8 ? 1 : keys <= 768 ? 4 : 0;
+  else gw = tiles <= 2 ? 1 : keys <= (real > 48 ? 1152 : 640) ? 4 : 0;
   CallResources res(stream);
   if (!workspace && gw == 0) {  // (one launch keeps nothing in it)
     if ((rc = res.alloc(paged_bytes(nw, M, D)))) return rc;
@@ -819,7 +829,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {
-      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)groups : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
+      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)(rounds == 1 ? groups : real) : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
       return hipGetLastError();
     });
   };

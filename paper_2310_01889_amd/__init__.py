@@ -584,8 +584,13 @@ def attention_decode(q, k_cache, v_cache, n_hosts, causal=True):
     return o, lse
 
 
-def paged_attention(q, k_pages, v_pages, block_table, lens, cu_rows=None, max_new=1, k_scales=None, v_scales=None):
-    """Returns (o [T, Hq, D] bf16, lse [T, Hq] f32) of paged_attn_decode, zeros in padding rows."""
+def paged_attention(q, k_pages, v_pages, block_table, lens, cu_rows=None, max_new=None, k_scales=None, v_scales=None):
+    """Returns (o [T, Hq, D] bf16, lse [T, Hq] f32) of paged_attn_decode, zeros in padding rows and in the
+    rows of a request past its first max_new; max_new goes with cu_rows (without them it is 1)."""
+    if max_new is None:
+        if cu_rows is not None:
+            raise ValueError("max_new, the most new tokens of a request, must be given with cu_rows")
+        max_new = 1
     o = torch.zeros_like(q)
     lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
     paged_attn_decode(q, k_pages, v_pages, block_table, lens, cu_rows, o, lse, max_new, k_scales, v_scales)

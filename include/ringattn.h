@@ -469,7 +469,7 @@ int paged_attn_decode(const void* q, const void* k_pages, const void* v_pages, c
  * scale is the smallest power of two (2^-126 at least) with which the group is at most 6 in
  * magnitude, codes are rounded to nearest, ties to the even code; a group with an infinity or NaN
  * has scale 255.
- * d_in % 32 == 0, d_in < 2^29, d_in * d_out < 2^31, T <= 512.  y may be residual; it overlaps no other input.
+ * d_in % 32 == 0, d_in <= 2^29 - 128, d_in * d_out < 2^31, T <= 512.  y may be residual; it overlaps no other input.
  */
 int mx4_pack(const void* w, void* w4, unsigned char* scales, int d_in, int d_out, hipStream_t stream);
 int mx4_linear(const void* x, const void* w4, const unsigned char* scales, const void* residual, void* y, int T,

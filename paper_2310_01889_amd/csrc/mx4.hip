@@ -209,7 +209,8 @@ __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
 int check_mx(int K, int N) {
   if (K <= 0 || N <= 0) return set_err(RA_EINVAL, "sizes must be positive (d_in=%d d_out=%d)", K, N);
   if (K % 32) return set_err(RA_EUNSUPPORTED, "d_in=%d must be a multiple of 32", K);
-  if (K >= 1 << 29) return set_err(RA_EUNSUPPORTED, "d_in=%d exceeds 2^29-1", K);  // 2^24 workgroups of the packing
+  // (the packing's grid: fewer than 2^24 workgroups of 256 threads)
+  if (K > (1 << 29) - 128) return set_err(RA_EUNSUPPORTED, "d_in=%d exceeds 2^29-128", K);
   if ((long long)K * N >= (1ll << 31)) return set_err(RA_EUNSUPPORTED, "d_in*d_out exceeds 2^31-1 elements");
   return RA_OK;
 }

@@ -213,8 +213,9 @@ struct AppendArgs {
 // A workgroup of 256 threads takes one token, 8 elements a thread of every head.  A thread's loads
 // (of kAppendLoads elements at a time) are issued before the token's cosines and sines are formed
 // into LDS, which hides one behind the other.  Angles: the turns position * freq in double, the
-// whole turns dropped, then sine and cosine of the rest in float32 (positions reach 10^6 radians
-// and more).  HBM-bound: 16384 tokens of 32 + 2 x 32 heads of 128 in bf16 (805 MB) 150 us.
+// whole turns dropped, sine and cosine of the rest in double, rounded once (positions reach 10^6
+// radians and more); with the rotation's products in the order that rope_apply's have, keys of one
+// token are the same from either.  HBM-bound: 16384 tokens of 32 + 2 x 32 heads of 128 in bf16 (805 MB) 150 us.
 constexpr int kAppendLoads = 4;
 
 template <int D, bool E4M3>
@@ -241,11 +242,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, c
     if (base == 0 && a.rotate) {
       if (threadIdx.x < D / 2) {
         const double turns = (double)pos * f.turns[threadIdx.x];
-        const float part = (float)(turns - rint(turns));
-        float sn, cs;
-        sincospif(2.f * part, &sn, &cs);
-        s_rope[2 * threadIdx.x] = cs;
-        s_rope[2 * threadIdx.x + 1] = sn;
+        double sn, cs;
+        sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
+        s_rope[2 * threadIdx.x] = (float)cs;
+        s_rope[2 * threadIdx.x + 1] = (float)sn;
       }
       __syncthreads();
     }
@@ -263,8 +263,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(const AppendArgs a, c
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float x0 = x[2 * e], x1 = x[2 * e + 1], c = cs[2 * e], s = cs[2 * e + 1];
-          x[2 * e] = x0 * c - x1 * s;
-          x[2 * e + 1] = x0 * s + x1 * c;
+          x[2 * e] = fmaf(x0, c, -(x1 * s));
+          x[2 * e + 1] = fmaf(x0, s, x1 * c);
         }
       }
       const long long row = (long long)slot * a.Hkv + h;

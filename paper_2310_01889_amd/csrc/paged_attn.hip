@@ -73,6 +73,8 @@ struct PagedArgs {
   int rounds;       // rounds of slots of a request at most
   int by_group;     // entries of split: 1 a group, 0 a wave
   int teams;        // workers / Hkv
+  int round_rows;   // one launch: rows a round holds at least, or 0: rounds of each request to a workgroup each
+  int rounds_row;   // rounds that a row takes at most
   float scale;
 };
 
@@ -183,18 +185,43 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
   int w = 0, team = 0, h, r, round = 0;
   long long share = 0, u0 = 0, u1 = 1, r_at = 0;  // r_at: first unit of request r
   Request q;                                      // request r
-  if (GW > 0 && a.rounds == 1) {  // a workgroup a (request, key head), of whatever requests have rows
-    r = id / a.Hkv;
-    h = id - r * a.Hkv;
+  if constexpr (GW > 0) {
+    if (a.round_rows == 0) {  // a workgroup a (request, key head, round), whether the request has it or not
+      const int g = id / a.rounds;
+      r = g / a.Hkv;
+      h = g - r * a.Hkv;
+      round = id - g * a.rounds;
+    } else {  // request r's rounds from number first(r) on: the largest r with first(r) <= u, 64 tried at a time
+      const int u = id / a.Hkv;
+      h = id - u * a.Hkv;
+      auto first = [&](int r) {
+        const int row = a.cu ? min(max(a.cu[r], 0), a.T) : r;
+        return G <= kSlots ? r + row / a.round_rows : row * a.rounds_row;
+      };
+      const int stride = (a.R + 63) / 64;
+      r = lane * stride;
+      r = max(0, __popcll(__builtin_amdgcn_ballot_w64(r < a.R && first(r) <= u)) - 1) * stride;
+      if (stride > 1) {
+        const int at = r + lane;
+        r += max(0, __popcll(__builtin_amdgcn_ballot_w64(lane < stride && at < a.R && first(at) <= u)) - 1);
+      }
+      r = __builtin_amdgcn_readfirstlane(r);
+      round = u - __builtin_amdgcn_readfirstlane(first(r));
+      if (round < 0) return;
+    }
     q = request(a, r);
   } else {
-    // ---- this team's share of the units, or the one (request, round) of a workgroup's heads ----
+    w = id * kShareWaves + wave;
+    team = w / a.Hkv;
+    h = w - team * a.Hkv;
+
+    // ---- this team's share of the units ----
     auto units = [&](int r, Request& q) -> long long {  // of request r
       q = Request{};
       if (r >= a.R) return 0;
       q = request(a, r);
       const int rounds = (q.n * G + kSlots - 1) / kSlots, tiles = max(1, (q.keys + KT - 1) / KT);
-      return GW > 0 ? rounds : (long long)rounds * tiles;
+      return (long long)rounds * tiles;
     };
     auto scan = [&](long long v) {  // inclusive prefix sum over the lanes
 #pragma unroll
@@ -208,21 +235,11 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     long long mine = 0;
     for (int j = 0; j < per; ++j) mine += units(lane * per + j, q);
     const long long upto = scan(mine), total = uniform(__shfl(upto, 63));
-    if constexpr (GW > 0) {
-      u0 = id / a.Hkv;
-      h = id - (int)u0 * a.Hkv;
-      u1 = u0 + 1;
-      if (u0 >= total) return;
-    } else {
-      w = id * kShareWaves + wave;
-      team = w / a.Hkv;
-      h = w - team * a.Hkv;
-      share = max(1ll, quotient(total + a.teams - 1, a.teams));
-      u0 = share * team;
-      u1 = min(total, u0 + share);
-      if (!a.by_group && lane == 0) a.split[w].parts = 0;
-      if (team >= a.teams || u0 >= u1) return;
-    }
+    share = max(1ll, quotient(total + a.teams - 1, a.teams));
+    u0 = share * team;
+    u1 = min(total, u0 + share);
+    if (!a.by_group && lane == 0) a.split[w].parts = 0;
+    if (team >= a.teams || u0 >= u1) return;
     // the request of unit u0: the lane whose sums reach past it, then the request among that lane's
     r = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(upto > u0)) - 1;
     r_at = __shfl(upto - mine, r);
@@ -241,7 +258,6 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
     q.n = __builtin_amdgcn_readlane(q.n, at);
     q.keys = __builtin_amdgcn_readlane(q.keys, at);
     q.first = __builtin_amdgcn_readlane(q.first, at);
-    if constexpr (GW > 0) round = (int)(u0 - r_at);
   }
 
   // ---- constants of the tile loop ----
@@ -790,11 +806,14 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   if (workspace && workspace_bytes < need)
     return set_err(RA_EINVAL, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   const long long groups = (long long)R * Hkv * rounds;
-  // Groups that the rows can make, whatever max_new allows (by rounds of slots): a round a request that has a row, and as 32 / G
-  // tokens are a round at most (a token G / 32, where G is larger), one for so many of the other rows.
-  const int some = std::min(R, T), G = Hq / Hkv;
-  const long long real = std::min(groups, Hkv * (long long)((G + kSlots - 1) / kSlots) *
-                                              (some + (T - some) / std::max(1, kSlots / G)));
+  // Groups that the rows can make, whatever max_new allows (by rounds of slots): rounds hold round_rows
+  // rows or more, so that n rows take 1 + (n - 1) / round_rows at most (a row of more slots than a round
+  // holds, rounds_row).  One launch gives request r as many as lie between first(r) and first(r + 1) in the
+  // kernel, which its first row says and which is no fewer.
+  const int some = std::min(R, T), G = Hq / Hkv, round_rows = std::max(1, kSlots / G), rounds_row = (G + kSlots - 1) / kSlots;
+  const long long real = std::min(groups, Hkv * (long long)rounds_row * (some + (T - some) / round_rows));
+  const long long numbers = Hkv * (G <= kSlots ? (long long)R + T / round_rows : (long long)T * rounds_row);
+  const bool by_rows = numbers < groups;
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
   // they do not and their turns take no longer than a second launch; else shares of all tiles and that
@@ -819,7 +838,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   }
   PagedArgs a{(const bf16*)q, k_pages, v_pages, k_scales, v_scales, block_table, lens, cu_rows, (bf16*)o, lse, nullptr,
               nullptr, nullptr, T, R, Hq, Hkv, n_pages, 0, max_pages, max_new, M, rounds, groups <= nw, nw / Hkv,
-              1.f / sqrtf((float)D)};
+              by_rows ? round_rows : 0, rounds_row, 1.f / sqrtf((float)D)};
   if (gw == 0) {
     a.part_acc = (float*)workspace;
     a.part_ml = a.part_acc + (size_t)nw * 2 * M * D;
@@ -829,7 +848,7 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {
-      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)(rounds == 1 ? groups : real) : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
+      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)(by_rows ? numbers : groups) : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
       return hipGetLastError();
     });
   };

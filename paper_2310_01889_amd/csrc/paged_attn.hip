@@ -456,10 +456,9 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
           thr = (m_new == -INFINITY) ? -INFINITY : kTau;
         }
         // Probabilities; the denominator sums them as they are, the products take them as the sum of
-        // three bf16 numbers, which is exact: the one next below, the one next below what that leaves,
-        // and the rest, 8 bits at most.  (With two they are off by up to 2^-16, which outputs that
-        // nearly cancel show.)  All three are above zero where the probability is, 2^-126 at least:
-        // an infinite value has an infinite sum (8 bits hold none).
+        // three bf16 numbers, the upper 8 bits of what the ones before leave: exact.  (With two they are
+        // off by up to 2^-16, which outputs that nearly cancel show.)  None is below 2^-126 where the
+        // probability is not: an infinite value has an infinite sum (8 bits hold none).
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
 #pragma unroll
@@ -482,12 +481,12 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
           for (int j = 0; j < 4; ++j) {
             float p0 = s[8 * g + 2 * j], p1 = s[8 * g + 2 * j + 1];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              w[e][j] = bf16x2_below(p0, p1);
-              p0 -= __uint_as_float(w[e][j] << 16);
-              p1 -= __uint_as_float(w[e][j] & 0xffff0000u);
+            for (int e = 0; e < 3; ++e) {
+              const uint32_t x = __float_as_uint(p0), y = __float_as_uint(p1);
+              w[e][j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+              p0 -= __uint_as_float(x & 0xffff0000u);
+              p1 -= __uint_as_float(y & 0xffff0000u);
             }
-            w[2][j] = pack_bf16x2(p0, p1);
             if constexpr (!F8) {
               const uint32_t least = min_u16x2(w[0][j], 0x800080u);
               w[1][j] = max_u16x2(w[1][j], least);

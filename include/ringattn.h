@@ -392,7 +392,8 @@ enum {
 /*
  * Pages, slots and positions of a step's new tokens, on the device (no host synchronisation).
  *   lens        in  int32 [R]  tokens in the cache;  n_new in int32 [R]  new tokens of this step
- *   free_pages  in  int32 [n_free]  ids of free pages, taken in order from entry *free_head on
+ *   free_pages  in  int32 [n_free]  ids of free pages, taken in order from entry *free_head on;
+ *               n_free >= 1 (an empty list: any one entry, with *free_head = 1)
  *   free_head   in  int32 [1], or NULL for 0; not inside counts
  *   block_table in/out int32 [R, max_pages]: request r holds ceil(lens[r] / page_size) pages; the
  *               entries of the pages it needs on top are written, in request order, no others
@@ -436,6 +437,9 @@ int paged_append(const void* q, const void* k, const void* v, void* q_out, void*
  *   lens       in  int32 [R]: tokens in the cache, this step's among them (new_lens of paged_plan)
  *   cu_rows    in  int32 [R + 1] ascending, or NULL: row r is the one new token of request r
  *   max_new    the most new tokens of a request, <= 32; later rows of a longer one are not computed
+ *   max_pages * page_size < 2^30.  How the work is split up goes by this product, the keys that a row of
+ *   the table can hold: where all requests are short, a table of no more columns than the longest
+ *   one needs is faster (16 groups of requests and key heads, 120 keys: 8 us for 11).
  *   Row t of the n of request r sits at position lens[r] - n + t and sees keys up to its own.
  *   Sums are float32 and relative to a maximum that may lag by up to 2^8: values of a magnitude
  *   past 2^119 divided by the number of keys may come out infinite.
@@ -443,7 +447,7 @@ int paged_append(const void* q, const void* k, const void* v, void* q_out, void*
  *   for nothing, whatever its row holds; a row that sees no key has o = 0, lse = -inf.  Rows of
  *   no request are left as they are.
  *   workspace  workspace_bytes of device memory on a 16-byte boundary, or NULL: allocated by the
- *              library like every other call's.  With a workspace of its own a call allocates
+ *              library like every other call's, if the call needs one.  With a workspace of its own a call allocates
  *              nothing and can be captured into a HIP graph; calls that may overlap, and graphs
  *              that may run at once, need one each.  Its contents before the call do not matter.
  * paged_attn_workspace gives the bytes that calls of this shape (and any lengths) need.

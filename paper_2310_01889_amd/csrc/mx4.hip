@@ -86,11 +86,14 @@ __device__ __forceinline__ bf16x8 from_e2m1(uint32_t codes, float scale) {
 // PIPE: codes and scales go through LDS as well and a wave has two stages, one in flight while the
 // other is computed; else weights go straight to registers and other waves hide the loads, eight
 // of them where their slabs are large (64 x 4096 x 4096 in 2 x 2 tiles: 6.7 us with two stages, 7.8 with
-// one; 24 x 4096 x 11008 in 2 x 4: 11.3 and 10.9).
+// one; 24 x 4096 x 11008 in 2 x 4: 11.3 and 10.9).  A wave of one stage waits for its own loads at
+// every 128 inputs.
 // Workgroups start at different inputs: the rows' pieces at one place lie in few channels of the L2
 // where the row length is a multiple of 4 KB (32 x 4096 x 4096: 7.6 us without, 6.7).
-// Bound by latency for few weights; by the weights' bytes; for many rows by what the compute units
-// take from L2, about 60 bytes a ns each, x being read whole by every column of workgroups.
+// Bound by latency for few weights; by the weights' bytes; for many rows by what the compute units take
+// from L2, x being read whole by every column of workgroups: 47 to 55 bytes a ns each with two stages (48 x
+// 11008 x 4096 in 2 x 2 0.89 MB in 16.2 us, in 1 x 4 0.73 in 15.5), 29 to 47 with one, where the loads are
+// waited for (24 x 4096 x 11008 in 2 x 3 0.30 MB in 10.3, 48 rows in 3 x 3 0.50 in 13.0).
 template <int NT, int NB, int WV, bool PIPE, int XL = 4 * NT>
 __global__ __launch_bounds__(64 * WV) void mx4_linear_kernel(const MxArgs a) {
   constexpr int SLAB = XL * 1024, STAGE = SLAB + (PIPE ? NB * 1280 : 0), LOADS = XL + 2 * NB;
@@ -245,15 +248,16 @@ extern "C" int mx4_linear(const void* x, const void* w4, const unsigned char* sc
            (d_in + 127) / 128};
   // Tiles NT and blocks NB a workgroup: the pair with which a compute unit (of 256) takes the fewest
   // bytes, counting for every input 8 of x for four rows and 17 a block of weights, twice what
-  // they are, for they come from memory and not from L2.  us of the pairs 1x1, 1x2, 1x4, 2x2, 2x4, 3x4:
-  //   32 x 4096 x 4096   7.5  5.2  6.8  6.7  -     -        20 x 4096 x 2048   4.6  4.9  6.6  6.2  -  -
-  //   48 x 11008 x 4096  20.6 18.6 15.6 15.6 20.6  -        48 x 4096 x 11008  -  15.8 17.2 16.9 16.5 13.2
-  //   96 x 4096 x 11008  -    25.9 25.3 24.5 20.6  21.0
-  // 4x4 for 64 x 4096 x 11008: 16.8 us, 2x4 17.9.  Three blocks where two need two rounds of the chip and
-  // four leave units idle: 7 x 4096 x 11008 7.2 us, 1x4 7.9; 24 x 4096 x 11008 10.1, 2x4 10.8; 48 rows 12.2, 3x4
-  // 13.3.  Several tiles of three and more blocks, one stage: eight waves where every workgroup has a compute
-  // unit of its own (24 x 4096 x 11008 10.9 us, four waves 15.4), else four, two workgroups a unit (300 x
-  // 4096 x 4096 18.3, eight waves 20.6).  1x1 and up to eight rows: 16 waves (1 x 11008 x 4096 6.6 us, eight
+  // they are, for they come from memory and not from L2.  us of a call among others, 512 MB of weights taken
+  // in turn so that they come from memory, by pair 1x1, 1x2, 1x4, 2x2, 2x4, 3x4 (a call alone is 5.7):
+  //   32 x 4096 x 4096   8.4  6.1  7.7  8.1  -     -        20 x 4096 x 2048   5.9  5.9  7.3  7.1  -  -
+  //   48 x 11008 x 4096  22.3 19.3 15.5 16.2 22.0  28.6     48 x 4096 x 11008  28.7 20.9 19.8 19.0 17.1 14.0
+  //   96 x 4096 x 11008  48.4 34.9 31.5 28.3 20.5  21.7
+  // 4x4 for 64 x 4096 x 11008: 17.4 us, 2x4 18.2.  Three blocks where two need two rounds of the chip and
+  // four leave units idle: 7 x 4096 x 11008 7.1 us, 1x4 7.8; 24 x 4096 x 11008 10.3, 2x4 11.2; 48 rows 13.0, 3x4
+  // 14.0.  Several tiles of three and more blocks, one stage: eight waves where every workgroup has a compute
+  // unit of its own (24 x 4096 x 11008 10.3 us, four waves 15.0), else four, two workgroups a unit (300 x
+  // 4096 x 4096 21.1, eight waves 22.7).  1x1 and up to eight rows: 16 waves (1 x 11008 x 4096 6.7 us, eight
   // waves 8.1).
   const int tiles = (T + 15) / 16, blocks = (d_out + 15) / 16;
   const int xl = T <= 4 ? 1 : T <= 8 ? 2 : 4;

@@ -32,14 +32,16 @@ constexpr int kSlots = 32;       // query slots a wave
 
 // Keys a tile, and the waves that share all tiles, four a workgroup: neighbouring key heads read pieces of
 // one token, so their waves stay close to one another in time and place (24 requests of 700 to 16001
-// tokens, us with one, two and four waves a workgroup: 8 heads of 128 dims in bf16 160-182, 152-156,
-// 152-154; 16 heads of 64 dims 168-180, 155-161, 152-157; 32 heads in 8 bits 346, 310, 294).
-// bf16: tiles of 8 KB, four of them (32 KB of LDS) a wave, four waves a compute unit (768 waves in
-// place of 1024: 163 us for 153; 262144 tokens of 32 heads 738 for 713).
+// tokens, one new each, us with one, two and four waves a workgroup: 8 heads of 128 dims in bf16 167, 159,
+// 157; 16 heads of 64 dims 177, 167, 162, in 8 bits 119, 121, 100; 8 heads of 128 in 8 bits 91, 92, 92).
+// bf16: tiles of 8 KB, four of them (32 KB of LDS) a wave, one workgroup a compute unit (768 waves in
+// place of 1024: 16 heads of 64 190 us for 162; 262144 tokens of 32 heads 728 for 707).
 // 8 bits: rows have half the bytes and the same products: 4 KB tiles, so that a SIMD's second wave
-// converts and multiplies while the first one waits (8 KB tiles and 1024 waves: 117 us for 98).
-// Seven waves a compute unit for 128 dims, whose partial states stay below 64 MB, eight for 64 (us
-// with 1280, 1536, 1792, 2048 waves: 8 heads of 128 106, 95, 91, 92; of 64 78, 71, 66, 62).
+// converts and multiplies while the first one waits (8 KB tiles and 1024 waves: 8 heads of 128 97 us
+// for 92, of 64 59 for 49).  Two workgroups fit a compute unit's LDS: 2048 waves fill the chip; for 128 dims
+// 1792 (448 workgroups: most units have two, some one), with which the partial states of 32 slots
+// stay below the 64 MB of a workspace that the library keeps (us with 1280, 1536, 1792, 2048 waves:
+// 8 heads of 128 112, 97, 90, 87; of 64 64, 59, 53, 49).
 // Four waves that join in LDS take 64 keys at a time in 8 bits as well, which is the room their states
 // need.
 constexpr int kShareWaves = 4;
@@ -152,13 +154,14 @@ __device__ __forceinline__ u32x4 only_finite(u32x4 x) {
 
 // GW = 0: each wave its team's share of all units.  GW > 0: short requests; GW waves take
 // the tiles of one group (request, key head, round) in turns and join their states in LDS, so that
-// one launch does.  Per tile the arithmetic of the decode kernel over a contiguous cache:
+// one launch does.  Per tile the arithmetic of the decode kernel over a contiguous cache, but for the
+// probabilities' parts:
 // S^T = K Q^T on the matrix cores (K rows with bits 2 and 3 of the row index swapped as the A
 // operand, a lane one query slot), lazy online softmax, O^T += V^T P^T with V^T from the
 // transpose reads of LDS.  Tiles are double buffered: the direct-to-LDS loads of tile i + 1,
 // every row at an address of its own (pages of any size), are in flight while tile i is computed.
 // 8-bit tiles become bf16 operands in registers, exactly: key rows under their scales, values as
-// they are, their scales (powers of two) going into the probabilities before those are rounded.
+// they are, their scales (powers of two) going into the probabilities before those are split.
 template <int D, bool F8, int GW>
 __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void paged_attn_kernel(const PagedArgs a) {
   constexpr int NW = GW ? GW : 1, WAVES = GW ? GW : kShareWaves;  // waves of a group, of a workgroup
@@ -817,14 +820,14 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
   // they do not and their turns take no longer than a second launch; else shares of all tiles and that
   // second launch.  us with one wave, four, shares; one token a request, of a quarter of the keys to all:
-  //   1024 groups of 128 dims in bf16: 120 keys 11.3, 19.0, 21.3; 500 31.9, 39.1, 38.0; 1000 68.0, 75.6,
-  //   64.8.  512 groups: 120 8.3, 9.9, 15.7; 500 25.8, 22.0, 24.9; 1000 45.1, 34.0, 35.8; 1500 64.4, 46.8,
-  //   44.7.  128 groups: 250 11.6, 7.9, 11.4; 1000 40.3, 17.1, 19.6; 1500 57.6, 23.5, 22.4; in 8 bits 1000
-  //   38.2, 15.1, 19.3; 2000 76.3, 25.2, 23.9.  16 groups: 120 7.9, 7.9, 11.2; 500 20.4, 9.9, 11.6; 1000
-  //   37.2, 15.9, 11.8.  256 groups of 64 dims in bf16: 500 14.3, 8.1, 14.1; 2000 52.3, 23.7, 24.3.
-  // Four waves, shares; of a third of the keys to all:  58 groups, one token 1000 16.3, 17.3; 1500 23.0, 17.3;
-  //   four tokens of 8 heads 1000 19.2, 27.3; 1500 25.4, 26.7.  32 groups 600 11.3, 12.4; 1000 15.8, 12.0.
-  //   320 groups, four tokens of 4 heads 600 25.7, 26.3; 1000 32.8, 30.2; in 8 bits 600 22.9, 24.7.
+  //   1024 groups of 128 dims in bf16: 120 keys 14.5, 22.4, 22.4; 500 39.2, 47.1, 40.2; 1000 78.4, 88.0,
+  //   72.0.  512 groups: 120 9.8, 10.6, 15.9; 500 31.1, 26.0, 26.6; 1000 55.7, 41.3, 35.8; 1500 79.3, 55.4,
+  //   45.7.  128 groups: 250 14.5, 8.1, 11.2; 1000 52.0, 18.7, 19.9; 1500 75.3, 25.2, 22.6; in 8 bits 1000
+  //   43.5, 15.8, 18.5; 2000 83.5, 28.2, 22.1.  16 groups: 120 8.8, 8.0, 11.4; 500 25.9, 10.7, 12.0; 1000
+  //   48.3, 17.4, 12.0.  256 groups of 64 dims in bf16: 500 17.6, 9.1, 14.6; 2000 61.4, 26.3, 25.6.
+  // Four waves, shares; of a third of the keys to all:  58 groups, one token 1000 18.3, 18.0; 1500 25.1, 17.6;
+  //   four tokens of 8 heads 1000 21.3, 33.4; 1500 27.9, 32.6.  32 groups 600 12.4, 12.5; 1000 17.3, 13.1.
+  //   320 groups, four tokens of 4 heads 600 30.0, 29.1; 1000 41.3, 33.4; in 8 bits 600 28.2, 27.2.
   const long long keys = (long long)max_pages * page_size, kt = f8 || D == 64 ? 64 : 32, tiles = (keys + kt - 1) / kt;
   int gw = 0;
   if (real >= 1024) gw = keys <= 768 ? 1 : 0;

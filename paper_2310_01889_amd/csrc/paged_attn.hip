@@ -460,8 +460,8 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
         }
         // Probabilities; the denominator sums them as they are, the products take them as the sum of
         // three bf16 numbers, the upper 8 bits of what the ones before leave: exact.  (With two they are
-        // off by up to 2^-16, which outputs that nearly cancel show.)  None is below 2^-126 where the
-        // probability is not: an infinite value has an infinite sum (8 bits hold none).
+        // off by up to 2^-16, which outputs that nearly cancel show.)  None is zero, but 2^-133 at least,
+        // where the probability is not: an infinite value has an infinite sum (8 bits hold none).
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = fast_exp2(s[i]);
 #pragma unroll
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
               p1 -= __uint_as_float(y & 0xffff0000u);
             }
             if constexpr (!F8) {
-              const uint32_t least = min_u16x2(w[0][j], 0x800080u);
+              const uint32_t least = min_u16x2(w[0][j], 0x10001u);
               w[1][j] = max_u16x2(w[1][j], least);
               w[2][j] = max_u16x2(w[2][j], least);
             }

@@ -66,3 +66,30 @@ def test_an_infinite_value_of_small_probability(wide):
     o, lse = call(s, 1)
     assert (o[0, 0, :n] == float("inf")).all() and (o[0, 0, 64:64 + n] == float("-inf")).all()
     assert (o[0, 0, n:64] == 1).all()
+
+
+def test_a_huge_value_of_small_probability():
+    """Zeros but for one value of 2^127 under a probability of 2^-106 to 2^-119: o is their product to bf16's
+    precision, as no part of a probability is moved by more than 2^-132: 2^-13 of it.
+
+    Scores are 0 and one product of two bf16 numbers, so the probability is 2^x with x rounded at 120:
+    2^-18 in x, 2^-18 ln 2 of the value, and the hardware's own 2^-23."""
+    D = 64
+    ks = [-range_ / 8 for range_ in range(108 * 8, 118 * 8)]
+    s = make(94, [2] * len(ks), [1] * len(ks), 1, 1, D, 16, False)
+    s["q"].zero_()
+    s["k"].zero_()
+    s["v"].zero_()
+    s["q"][:, 0, 0] = 8.0
+    for r, x in enumerate(ks):
+        i = s["table_np"][r, 0]
+        s["k"][i, 1, 0, 0] = x * 0.6931  # times 8 / sqrt(64)
+        s["v"][i, 1, 0, 3] = 2.0 ** 127
+    o, lse = call(s, 1)
+    k = np64(torch.stack([s["k"][s["table_np"][r, 0], 1, 0, 0] for r in range(len(ks))]))
+    want = np.exp(k) * 2.0 ** 127
+    assert (np.exp(k) > 2.0 ** -119).all() and (np.exp(k) < 2.0 ** -106).all()
+    err = np.abs(np64(o)[:, 0, 3] / want - 1)
+    log("  relative error %.2e, bf16 rounds by up to %.2e" % (err.max(), 2.0 ** -8))
+    assert (err <= 2.0 ** -8 + 2.0 ** -13 + 2.0 ** -18 + 2.0 ** -22).all()
+    assert (np64(o)[:, 0, :3] == 0).all()

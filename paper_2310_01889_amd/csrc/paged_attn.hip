@@ -201,14 +201,17 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
         const int row = a.cu ? min(max(a.cu[r], 0), a.T) : r;
         return G <= kSlots ? r + row / a.round_rows : row * a.rounds_row;
       };
-      const int stride = (a.R + 63) / 64;
-      r = lane * stride;
-      r = max(0, __popcll(__builtin_amdgcn_ballot_w64(r < a.R && first(r) <= u)) - 1) * stride;
+      auto last = [](bool on) -> int {  // of the lanes from 0 on where it is true; 0 if it is nowhere
+        const int n = (int)__popcll(__builtin_amdgcn_ballot_w64(on));  // (unsigned as it comes)
+        return n > 0 ? n - 1 : 0;
+      };
+      const int stride = (a.R + 63) / 64, from = lane * stride;
+      r = last(from < a.R && first(from) <= u) * stride;
       if (stride > 1) {
         const int at = r + lane;
-        r += max(0, __popcll(__builtin_amdgcn_ballot_w64(lane < stride && at < a.R && first(at) <= u)) - 1);
+        r += last(lane < stride && at < a.R && first(at) <= u);
       }
-      r = __builtin_amdgcn_readfirstlane(r);
+      r = __builtin_amdgcn_readfirstlane(min(r, a.R - 1));
       round = u - __builtin_amdgcn_readfirstlane(first(r));
       if (round < 0) return;
     }

@@ -198,7 +198,7 @@ __global__ __launch_bounds__(64 * (GW ? GW : kShareWaves), GW > 1 ? 1 : 2) void 
       const int u = id / a.Hkv;
       h = id - u * a.Hkv;
       auto first = [&](int r) {
-        const int row = a.cu ? min(max(a.cu[r], 0), a.T) : r;
+        const int row = min(max(a.cu[r], 0), a.T);
         return G <= kSlots ? r + row / a.round_rows : row * a.rounds_row;
       };
       auto last = [](bool on) -> int {  // of the lanes from 0 on where it is true; 0 if it is nowhere
@@ -815,10 +815,11 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   // rows or more, so that n rows take 1 + (n - 1) / round_rows at most (a row of more slots than a round
   // holds, rounds_row).  One launch gives request r as many as lie between first(r) and first(r + 1) in the
   // kernel, which its first row says and which is no fewer.
-  const int some = std::min(R, T), G = Hq / Hkv, round_rows = std::max(1, kSlots / G), rounds_row = (G + kSlots - 1) / kSlots;
+  const int some = std::min(R, T), G = Hq / Hkv;
+  const int round_rows = std::max(1, kSlots / G), rounds_row = (G + kSlots - 1) / kSlots;
   const long long real = std::min(groups, Hkv * (long long)rounds_row * (some + (T - some) / round_rows));
   const long long numbers = Hkv * (G <= kSlots ? (long long)R + T / round_rows : (long long)T * rounds_row);
-  const bool by_rows = numbers < groups;
+  const bool by_rows = numbers < groups;  // (never without cu_rows: max_new is 1 then)
   // Short requests, by what their tables can hold: one launch, a workgroup a group.  One wave each
   // where the groups fill the chip or the tiles (64 keys, 32 of 256-byte rows) are few, four waves where
   // they do not and their turns take no longer than a second launch; else shares of all tiles and that
@@ -852,8 +853,9 @@ extern "C" int paged_attn_decode(const void* q, const void* k_pages, const void*
   while ((1 << a.page_shift) < page_size) ++a.page_shift;
   auto launch = [&](auto* share, auto* one, auto* four) {
     auto* kern = gw == 0 ? share : gw == 1 ? one : four;
+    const unsigned grid = gw == 0 ? nw / kShareWaves : (unsigned)(by_rows ? numbers : groups);
     return timed_launch(RA_KERNEL_DECODE, stream, [&] {
-      hipLaunchKernelGGL(kern, dim3(gw ? (unsigned)(by_rows ? numbers : groups) : nw / kShareWaves), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
+      hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * (gw ? gw : kShareWaves)), 0, stream, a);
       return hipGetLastError();
     });
   };
